@@ -98,9 +98,12 @@ enum { CHIMERA_REFINE_CENTROID = 0, CHIMERA_REFINE_TOKEN = 1 };
 #define CHIMERA_MAX_NPROBE 64
 #define CHIMERA_MAX_NCAND (1 << 20)
 #define CHIMERA_MAX_K 8192
+#define CHIMERA_PAGES_MAX_LEN (1 << 20)   /* tokens of a document of a paged store */
+#define CHIMERA_PAGES_MAX_SCORE (1 << 28) /* documents scored for a query in one call */
 
 typedef struct chimera_index chimera_index;
 typedef struct chimera_builder chimera_builder;
+typedef struct chimera_pages chimera_pages;
 
 typedef struct {
   int64_t ndocs;         /* documents */
@@ -401,6 +404,128 @@ int chimera_search_collab(chimera_index *idx, const void *Q, int q_dtype, int64_
 int chimera_search_collab_rabitq(chimera_index *idx, const void *Q, int q_dtype, int64_t nq, int32_t Tq, int32_t d,
                                  int32_t nprobe, int32_t ncand, int32_t kfb, int32_t chunks, int32_t k, int32_t *ids,
                                  float *scores, int32_t *n_full, int32_t nthreads, void *hip_stream);
+
+/* ===================================================================== *
+ * Paged token store in MXFP4 (Sec. 3.3, handling updates: new documents,
+ * documents that grow or are revised, documents that go).
+ *
+ * The index is built once from the whole corpus; a paged store takes token
+ * vectors as an encoder leaves them in device memory, quantises them on the
+ * GPU into a third code family and holds them so that documents can be
+ * added, extended, shared, copied, compacted and dropped at any time, and
+ * scored by Chamfer similarity (Def. 1) straight from the codes.
+ *
+ *  - Codes: MXFP4, the microscaling format of 4-bit floats.  Each token's 128
+ *    values x are 4 blocks of 32.  With E the exponent field of the block's
+ *    largest |x| as a float32, the block's scale is X = 2^(s - 127), s =
+ *    max(E - 2, 0), and an element is the value of {0, 0.5, 1, 1.5, 2, 3, 4, 6}
+ *    nearest to |x| / X, ties to the even code (0, 1, 2, 4), above 6: 6, with
+ *    the sign of x.  A block with an infinity or a NaN becomes NaN (s = 255).
+ *    64 bytes of codes and 4 of scales a token.
+ *  - Pages: 16 tokens, 1088 bytes.  A store has npages of them for ndocs
+ *    documents, ids 0 .. ndocs - 1, each of at most max_len tokens, all empty
+ *    at first.  Token i of a document is slot i % 16 of its page i / 16; whole
+ *    pages can be shared by several documents (fork), a partly filled one
+ *    never is.  A document's pages need not be neighbours.
+ *  - Document ids given to append, fork, copy, drop, read and lengths are HOST
+ *    arrays; the store's host bookkeeping validates them, so these calls
+ *    fail before anything is launched or changed: E_INVAL for ids out of
+ *    range, for an id that is written twice in a call (drop and read allow
+ *    repeats) and for lengths out of range, E_NOMEM if the store has too few
+ *    free pages.  The arrays may be reused as soon as the call returns.
+ *  - Every call but create, free, info_get and lengths is asynchronous on
+ *    hip_stream and comes after all earlier calls on the store, whatever
+ *    their streams.  Tensors handed in (X, Q, the score's doc_ids) are read and
+ *    outputs written on hip_stream alone.  Only chimera_pages_score can be
+ *    captured into a graph (the others return E_UNSUPPORTED: their bookkeeping
+ *    would happen once); a captured score and its replays are not ordered by
+ *    the library: the caller keeps them apart from calls that change the
+ *    store and run on other streams.  A replay scores the documents as they
+ *    are when it runs.  A search (chimera_search_pages) cannot be captured.
+ *  - Concurrent host calls on one store return E_BUSY; info_get and lengths
+ *    must not overlap a call that changes the store.  After E_DEVICE the store
+ *    must be freed.
+ * ===================================================================== */
+
+typedef struct {
+  int64_t npages;       /* pages of the store */
+  int64_t free_pages;   /* pages that no document holds */
+  int64_t ndocs;        /* document ids */
+  int64_t ntokens;      /* tokens of all documents (shared ones counted for each) */
+  int64_t device_bytes; /* device memory of the store: 1088 npages + 4 ndocs (1 + ceil(max_len / 16)) */
+  int32_t max_len;      /* tokens a document can have */
+  int32_t device;       /* HIP device ordinal */
+} chimera_pages_info;
+
+/* npages, ndocs 1 .. 2^31 - 1, max_len 1 .. CHIMERA_PAGES_MAX_LEN.  Host memory:
+ * 8 npages + 4 ndocs (2 + ceil(max_len / 16)) bytes. */
+int chimera_pages_create(int hip_device, int64_t npages, int64_t ndocs, int32_t max_len, chimera_pages **out);
+void chimera_pages_free(chimera_pages *pg); /* NULL-safe; waits for pending work */
+int chimera_pages_info_get(const chimera_pages *pg, chimera_pages_info *out);
+/* lens host [n]: the documents' tokens. */
+int chimera_pages_lengths(const chimera_pages *pg, const int64_t *doc_ids, int64_t n, int32_t *lens);
+
+/* Quantises lens[i] >= 0 tokens to the end of document doc_ids[i] (distinct).
+ * X device, rows of d = 128 values (CHIMERA_F32 or CHIMERA_BF16), ld values
+ * from one to the next (X 16-byte aligned, ld a multiple of 16 bytes).
+ * doc_stride 0: the documents' rows follow one another (sum lens rows).
+ * doc_stride > 0: document i's rows are i * doc_stride and following (a padded
+ * batch; lens[i] <= doc_stride), what stands behind them is not read. */
+int chimera_pages_append(chimera_pages *pg, const int64_t *doc_ids, const int32_t *lens, int64_t n, const void *X,
+                         int x_dtype, int32_t d, int64_t ld, int64_t doc_stride, void *hip_stream);
+
+/* Document dst_ids[i] (empty, distinct, no source of this call) becomes the
+ * first lens[i] tokens of document src_ids[i] (lens NULL: all of them).  Whole
+ * pages are shared, the tokens behind them (fewer than 16) are copied to one
+ * new page, so either document can be extended or dropped afterwards without
+ * the other one changing.  A source may be named more than once. */
+int chimera_pages_fork(chimera_pages *pg, const int64_t *src_ids, const int64_t *dst_ids, const int32_t *lens,
+                       int64_t n, void *hip_stream);
+
+/* Document dst_ids[i] of dst becomes a copy, in pages of its own, of lens[i]
+ * tokens of document src_ids[i] of src (the same store or another one on the
+ * same device): those at positions (host, sum lens entries, one document behind
+ * the other, ascending within a document), or the first lens[i] where positions
+ * is NULL (lens NULL: all).  dst_ids are distinct and empty, but a document of
+ * the same store may be copied onto itself: the tokens that are not named go,
+ * the rest is packed into as few pages as hold it (compaction), and the old
+ * pages are free after the call.  The new pages must be free before the call. */
+int chimera_pages_copy(chimera_pages *src, const int64_t *src_ids, chimera_pages *dst, const int64_t *dst_ids,
+                       const int32_t *lens, const int32_t *positions, int64_t n, void *hip_stream);
+
+/* Empties documents (repeats and empty ones are allowed).  A page is free again
+ * when no document holds it. */
+int chimera_pages_drop(chimera_pages *pg, const int64_t *doc_ids, int64_t n, void *hip_stream);
+
+/* out device [sum of lengths][128], CHIMERA_F32 or CHIMERA_BF16 (both hold every
+ * value exactly), 16-byte aligned: the documents' values, one document behind
+ * the other (repeats are allowed). */
+int chimera_pages_read(chimera_pages *pg, const int64_t *doc_ids, int64_t n, void *out, int dtype, void *hip_stream);
+
+/* scores device [nq][n] float32: score(i, V) = sum_j max_{t in V} <Q_ij, v_t>
+ * over the stored values v of document V = doc_ids[i * ld + c].
+ *   Q        device [nq][Tq][128], 16-byte aligned, rounded onto the value grid
+ *            as for the searches; finite values
+ *   doc_ids  device [nq] lists of n ids, ld entries apart (0: one list for
+ *            every query); NULL: documents 0 .. n - 1, n <= ndocs
+ * An id outside [0, ndocs), an empty document and one whose tokens are all NaN
+ * score -infinity; a token with a NaN block is never a document's best.  Query
+ * values are used exactly while those of a block of 32 stay below 8 in
+ * magnitude (above, to within 2^-15 of the block's largest); products are summed
+ * in float32, as are the at most 64 maxima.  Neither scratch nor host
+ * synchronisation. */
+int chimera_pages_score(chimera_pages *pg, const void *Q, int q_dtype, int64_t nq, int32_t Tq, int32_t d,
+                        const int32_t *doc_ids, int64_t n, int64_t ld, float *scores, void *hip_stream);
+
+/* chimera_search with step 4 scored from a paged store: the kept documents of
+ * the index are ranked by score(i, V) of the documents of the same ids in pg
+ * (same device; pg's ndocs >= the index's), through the keys rint(score 2^22)
+ * (saturating at +-2^31); scores are key * 2^-22 in float32.  Kept documents
+ * that score -infinity (no tokens in pg) are left out: the results end in
+ * (-1, -INFINITY) there. */
+int chimera_search_pages(chimera_index *idx, chimera_pages *pg, const void *Q, int q_dtype, int64_t nq, int32_t Tq,
+                         int32_t d, int32_t nprobe, int32_t ncand, int32_t k, int32_t *ids, float *scores,
+                         void *hip_stream);
 
 /* Stage taps: the same inputs as chimera_search, stopping after a stage.
  * They exist so that each stage can be compared with an independent

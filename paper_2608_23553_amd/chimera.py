@@ -7,6 +7,7 @@ of this module still works, but every call raises ``RuntimeError``.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Callable, Iterable, Tuple
@@ -35,6 +36,12 @@ class _Info(ctypes.Structure):
                 ("ncent", ctypes.c_int32), ("dim", ctypes.c_int32), ("nbits", ctypes.c_int32),
                 ("max_doc_len", ctypes.c_int32), ("device_bytes", ctypes.c_int64), ("device", ctypes.c_int32),
                 ("q_norm_limit", ctypes.c_double), ("ndeleted", ctypes.c_int64)]
+
+
+class _PagesInfo(ctypes.Structure):
+    _fields_ = [("npages", ctypes.c_int64), ("free_pages", ctypes.c_int64), ("ndocs", ctypes.c_int64),
+                ("ntokens", ctypes.c_int64), ("device_bytes", ctypes.c_int64), ("max_len", ctypes.c_int32),
+                ("device", ctypes.c_int32)]
 
 
 def lib():
@@ -78,6 +85,17 @@ def lib():
         "chimera_fullbit_attach": ([P, P, I64], INT),
         "chimera_fullbit_attach_range": ([P, P, I64, I64], INT),
         "chimera_search_collab": ([P, P, INT, I64, I32, I32, I32, I32, I32, I32, I32, P, P, P, I32, P], INT),
+        "chimera_pages_create": ([INT, I64, I64, I32, P], INT),
+        "chimera_pages_free": ([P], None),
+        "chimera_pages_info_get": ([P, P], INT),
+        "chimera_pages_lengths": ([P, P, I64, P], INT),
+        "chimera_pages_append": ([P, P, P, I64, P, INT, I32, I64, I64, P], INT),
+        "chimera_pages_fork": ([P, P, P, P, I64, P], INT),
+        "chimera_pages_copy": ([P, P, P, P, P, P, I64, P], INT),
+        "chimera_pages_drop": ([P, P, I64, P], INT),
+        "chimera_pages_read": ([P, P, I64, P, INT, P], INT),
+        "chimera_pages_score": ([P, P, INT, I64, I32, I32, P, I64, I64, P, P], INT),
+        "chimera_search_pages": ([P, P, P, INT, I64, I32, I32, I32, I32, I32, P, P, P], INT),
         "chimera_search_collab_rabitq": ([P, P, INT, I64, I32, I32, I32, I32, I32, I32, I32, P, P, P, I32, P],
                                          INT),
     }
@@ -105,8 +123,8 @@ def _np(a: np.ndarray | None):
     return ctypes.c_void_p(a.ctypes.data)
 
 
-def _info(st: _Info) -> dict:
-    return {k: getattr(st, k) for k, _ in _Info._fields_}
+def _info(st) -> dict:
+    return {k: getattr(st, k) for k, _ in st._fields_}
 
 
 # --------------------------------------------------------------- builder
@@ -229,10 +247,10 @@ def build_index(centroids_bf16: np.ndarray, nbits: int,
 
 
 # ----------------------------------------------------------------- index
-def _stream_ptr(stream) -> ctypes.c_void_p:
+def _stream_ptr(stream, device=None) -> ctypes.c_void_p:
     import torch
     if stream is None:
-        stream = torch.cuda.current_stream()
+        stream = torch.cuda.current_stream(device)
     return ctypes.c_void_p(stream.cuda_stream)
 
 
@@ -303,21 +321,25 @@ class Index:
         import torch
         return torch.device("cuda", self._info["device"])
 
+    def _results(self, Q, nq, k, out):
+        """The tensors of a search's results: new ones, or out's, checked."""
+        import torch
+        if out is None:
+            return (torch.empty((nq, k), dtype=torch.int32, device=Q.device),
+                    torch.empty((nq, k), dtype=torch.float32, device=Q.device))
+        ids, scores = out
+        for t, dtype, name in ((ids, torch.int32, "ids"), (scores, torch.float32, "scores")):
+            if tuple(t.shape) != (nq, k) or t.dtype != dtype or t.device != Q.device or not t.is_contiguous():
+                raise ValueError(f"out {name} must be a contiguous {dtype} tensor [{nq}, {k}] on {Q.device}")
+        return ids, scores
+
     def search(self, Q, nprobe: int, ncand: int, k: int, out=None, stream=None, refine: int = REFINE_CENTROID):
         """Top-k (ids int32 [nq,k], scores float32 [nq,k]) for queries Q [nq,Tq,d].
         refine: REFINE_CENTROID (chimera_search) or REFINE_TOKEN
         (chimera_search_refine)."""
-        import torch
         Q, dt = self._q(Q)
         nq, Tq, d = Q.shape
-        if out is None:
-            ids = torch.empty((nq, k), dtype=torch.int32, device=Q.device)
-            scores = torch.empty((nq, k), dtype=torch.float32, device=Q.device)
-        else:
-            ids, scores = out
-            for t, dtype, name in ((ids, torch.int32, "ids"), (scores, torch.float32, "scores")):
-                if tuple(t.shape) != (nq, k) or t.dtype != dtype or t.device != Q.device or not t.is_contiguous():
-                    raise ValueError(f"out {name} must be a contiguous {dtype} tensor [{nq}, {k}] on {Q.device}")
+        ids, scores = self._results(Q, nq, k, out)
         if refine == REFINE_CENTROID:
             _check(lib().chimera_search(self._h, ctypes.c_void_p(Q.data_ptr()), dt, nq, Tq, d, nprobe, ncand, k,
                                         ctypes.c_void_p(ids.data_ptr()), ctypes.c_void_p(scores.data_ptr()),
@@ -341,6 +363,15 @@ class Index:
         _check(lib().chimera_search_rabitq(self._h, ctypes.c_void_p(Q.data_ptr()), dt, nq, Tq, d, nprobe, ncand, k,
                                            ctypes.c_void_p(ids.data_ptr()), ctypes.c_void_p(scores.data_ptr()),
                                            _stream_ptr(stream)))
+        return ids, scores
+
+    def search_pages(self, pages: "Pages", Q, nprobe: int, ncand: int, k: int, out=None, stream=None):
+        """chimera_search_pages: step 4 scored from a paged store's documents of the same ids."""
+        Q, dt = self._q(Q)
+        nq, Tq, d = Q.shape
+        ids, scores = self._results(Q, nq, k, out)
+        _check(lib().chimera_search_pages(self._h, pages._h, _aligned(Q).data_ptr(), dt, nq, Tq, d, nprobe, ncand, k,
+                                          ids.data_ptr(), scores.data_ptr(), _stream_ptr(stream)))
         return ids, scores
 
     def attach_fullbit(self, tokens_bf16):
@@ -449,3 +480,190 @@ class Index:
         ms = np.zeros(7, np.float32)
         _check(lib().chimera_stage_times(self._h, _np(ms)))
         return ms
+
+
+# ----------------------------------------------------------------- pages
+def _aligned(t):
+    """t, or a copy where its first value is not 16-byte aligned, as the library asks."""
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
+def _on(stream):
+    """Where a call's own tensors are made: on its stream, so that copies are in order with the call and the memory
+    is not given away while it runs."""
+    import torch
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _ids(ids) -> np.ndarray:
+    a = np.asarray(ids)
+    if a.dtype != np.int64 and a.size and a.dtype.kind not in "iu":
+        raise ValueError(f"document ids must be whole numbers, got {a.dtype}")
+    a = np.ascontiguousarray(a, dtype=np.int64)
+    return a if a.ndim == 1 else a.reshape(-1)
+
+
+def _counts(a, n: int | None, name: str) -> np.ndarray:
+    """Lengths or positions as int32 [n]; a value that int32 does not hold is an error, not another value."""
+    b = np.asarray(a)
+    if b.dtype != np.int32:
+        if b.size and (b.dtype.kind not in "iu" or b.max() > 2**31 - 1 or b.min() < -2**31):
+            raise ValueError(f"{name} must be whole numbers of 32 bits")
+        b = b.astype(np.int32)
+    if b.ndim != 1 or (n is not None and b.shape[0] != n):
+        raise ValueError(f"{name} must be [{'n' if n is None else n}], got {list(b.shape)}")
+    return np.ascontiguousarray(b)
+
+
+class Pages:
+    """A paged store of documents' token vectors in MXFP4 (``chimera_pages_create``): npages pages of 16 tokens for
+    documents 0 .. ndocs - 1 of at most max_len tokens each, all empty at first.  Document ids, lengths and positions
+    are host arrays or lists; token vectors, queries and results are device tensors."""
+
+    def __init__(self, npages: int, ndocs: int, max_len: int, device: int = 0):
+        h = ctypes.c_void_p()
+        _check(lib().chimera_pages_create(device, npages, ndocs, max_len, ctypes.byref(h)))
+        self._h = h
+        self.ndocs, self.max_len, self.device_index = ndocs, max_len, device
+
+    def close(self):
+        if getattr(self, "_h", None) and _lib is not None:
+            _lib.chimera_pages_free(self._h)
+            self._h = None
+
+    def __del__(self):
+        self.close()
+
+    def info(self) -> dict:
+        st = _PagesInfo()
+        _check(lib().chimera_pages_info_get(self._h, ctypes.byref(st)))
+        return _info(st)
+
+    @property
+    def device(self):
+        import torch
+        return torch.device("cuda", self.device_index)
+
+    def _tensor(self, t, name):
+        """A float32 or bfloat16 tensor on the store's own GPU, and its type for the library."""
+        import torch
+        if not t.is_cuda or t.device.index != self.device_index:
+            raise ValueError(f"{name} is on {t.device}, the pages on cuda:{self.device_index}")
+        if t.dtype == torch.float32:
+            return F32
+        if t.dtype == torch.bfloat16:
+            return BF16
+        raise ValueError(f"{name} must be float32 or bfloat16")
+
+    def lengths(self, ids=None) -> np.ndarray:
+        """Tokens of each document of ids (all documents)."""
+        a = np.arange(self.ndocs, dtype=np.int64) if ids is None else _ids(ids)
+        out = np.empty(a.size, np.int32)
+        _check(lib().chimera_pages_lengths(self._h, a.ctypes.data, a.size, out.ctypes.data))
+        return out
+
+    def append(self, ids, X, lens=None, stream=None):
+        """Quantises tokens to the ends of documents (chimera_pages_append).  X [rows, 128] holds lens[i] rows for each
+        document, one behind the other; X [n, L, 128] is a padded batch, of which document i takes the first lens[i]
+        rows (lens None: all L)."""
+        dt = self._tensor(X, "X")
+        a = _ids(ids)
+        if X.dim() == 3:
+            if X.shape[0] != a.size:
+                raise ValueError(f"X must be [{a.size}, L, 128], got {list(X.shape)}")
+            lens = np.full(a.size, X.shape[1], np.int32) if lens is None else _counts(lens, a.size, "lens")
+            if lens.size and lens.max() > X.shape[1]:
+                raise ValueError(f"lens must be at most {X.shape[1]}, the batch's padded length")
+        elif X.dim() == 2:
+            if lens is None:
+                raise ValueError("lens is needed with X [rows, 128]")
+            lens = _counts(lens, a.size, "lens")
+            if int(lens.sum(dtype=np.int64)) != X.shape[0]:
+                raise ValueError(f"lens sum up to {int(lens.sum(dtype=np.int64))}, X has {X.shape[0]} rows")
+        else:
+            raise ValueError("X must be [rows, 128] or [n, L, 128]")
+        # rows may be strided, a batch's documents too as long as its rows are evenly spaced
+        unit = 4 if dt == F32 else 8
+        ld = X.stride(-2)
+        doc = X.shape[1] if X.dim() == 3 else 0
+        if (X.stride(-1) != 1 or ld % unit or ld < X.shape[-1] or X.data_ptr() % 16
+                or (X.dim() == 3 and X.shape[0] > 1 and X.stride(0) != X.shape[1] * ld)):
+            with _on(stream):
+                X = _aligned(X.contiguous())
+            ld = X.shape[-1]
+        _check(lib().chimera_pages_append(self._h, a.ctypes.data, lens.ctypes.data, a.size, X.data_ptr(), dt,
+                                          X.shape[-1], ld, doc, _stream_ptr(stream, self.device_index)))
+
+    def fork(self, src, dst, lens=None, stream=None):
+        """Documents dst (empty) become the first lens[i] tokens (None: all) of documents src, sharing their whole
+        pages (chimera_pages_fork)."""
+        a, b = _ids(src), _ids(dst)
+        if a.size != b.size:
+            raise ValueError(f"{a.size} sources for {b.size} documents")
+        lens = None if lens is None else _counts(lens, a.size, "lens")
+        _check(lib().chimera_pages_fork(self._h, a.ctypes.data, b.ctypes.data, _np(lens), a.size, _stream_ptr(stream, self.device_index)))
+
+    def copy(self, src, dst, lens=None, positions=None, to: "Pages" | None = None, stream=None):
+        """Documents dst (empty, or the source itself) of `to` (None: this store) become copies, in pages of their own,
+        of lens[i] tokens of documents src: the first ones, or those at positions, ascending for each document and one
+        document's behind the other's (chimera_pages_copy)."""
+        a, b = _ids(src), _ids(dst)
+        if a.size != b.size:
+            raise ValueError(f"{a.size} sources for {b.size} documents")
+        lens = None if lens is None else _counts(lens, a.size, "lens")
+        if positions is not None:
+            if lens is None:
+                raise ValueError("lens is needed with positions")
+            positions = _counts(positions, int(lens.sum(dtype=np.int64)), "positions")
+        _check(lib().chimera_pages_copy(self._h, a.ctypes.data, (to or self)._h, b.ctypes.data, _np(lens),
+                                        _np(positions), a.size, _stream_ptr(stream, self.device_index)))
+
+    def drop(self, ids, stream=None):
+        """Empties documents (chimera_pages_drop)."""
+        a = _ids(ids)
+        _check(lib().chimera_pages_drop(self._h, a.ctypes.data, a.size, _stream_ptr(stream, self.device_index)))
+
+    def read(self, ids, dtype=None, out=None, stream=None):
+        """The stored values of documents, one behind the other: [sum of lengths, 128], bfloat16 unless dtype says
+        float32 (chimera_pages_read)."""
+        import torch
+        a = _ids(ids)
+        rows = int(self.lengths(a).sum(dtype=np.int64))
+        if out is None:
+            with _on(stream):
+                out = torch.empty((rows, 128), dtype=dtype or torch.bfloat16, device=self.device)
+        elif tuple(out.shape) != (rows, 128) or not out.is_contiguous() or (dtype is not None and out.dtype != dtype):
+            raise ValueError(f"out must be a contiguous tensor [{rows}, 128]{'' if dtype is None else f' of {dtype}'}")
+        dt = self._tensor(out, "out")
+        _check(lib().chimera_pages_read(self._h, a.ctypes.data, a.size, out.data_ptr(), dt, _stream_ptr(stream, self.device_index)))
+        return out
+
+    def score(self, Q, ids=None, out=None, stream=None):
+        """Scores float32 [nq, n] of queries Q [nq, Tq, 128] with stored documents (chimera_pages_score): ids int32 on
+        the GPU, [nq, n] a list for each query or [n] one for all; None: every document 0 .. ndocs - 1."""
+        import torch
+        dt = self._tensor(Q, "Q")
+        if Q.dim() != 3:
+            raise ValueError("Q must be [nq, Tq, d]")
+        with _on(stream):
+            Q = _aligned(Q.contiguous())
+        nq, Tq, d = Q.shape
+        n, ld = self.ndocs, 0
+        if ids is not None:
+            if ids.dtype != torch.int32 or ids.device != Q.device or ids.dim() not in (1, 2):
+                raise ValueError(f"ids must be an int32 tensor [n] or [{nq}, n] on {Q.device}")
+            if ids.dim() == 2 and ids.shape[0] != nq:
+                raise ValueError(f"ids must be [{nq}, n], got {list(ids.shape)}")
+            n = ids.shape[-1]
+            if ids.stride(-1) != 1 or (ids.dim() == 2 and nq > 1 and ids.stride(0) < n):
+                with _on(stream):
+                    ids = ids.contiguous()
+            ld = ids.stride(0) if ids.dim() == 2 and nq > 1 else 0
+        if out is None:
+            with _on(stream):
+                out = torch.empty((nq, n), dtype=torch.float32, device=Q.device)
+        elif tuple(out.shape) != (nq, n) or out.dtype != torch.float32 or out.device != Q.device or not out.is_contiguous():
+            raise ValueError(f"out must be a contiguous float32 tensor [{nq}, {n}] on {Q.device}")
+        _check(lib().chimera_pages_score(self._h, Q.data_ptr(), dt, nq, Tq, d, None if ids is None else ids.data_ptr(),
+                                         n, ld, out.data_ptr(), _stream_ptr(stream, self.device_index)))
+        return out

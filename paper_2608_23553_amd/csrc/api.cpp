@@ -8,7 +8,9 @@
 #include <cstring>
 #include <new>
 
+#include "guards.h"
 #include "internal.h"
+#include "pages_handle.h"
 
 namespace chimera {
 
@@ -26,28 +28,6 @@ int hip_fail(hipError_t e, const char *what) {
   if (e == hipErrorOutOfMemory) return fail(CHIMERA_E_NOMEM, "%s: %s", what, hipGetErrorString(e));
   return fail(CHIMERA_E_DEVICE, "%s: %s", what, hipGetErrorString(e));
 }
-
-// Restores the caller's current device on scope exit.
-struct DeviceGuard {
-  int prev = -1;
-  bool ok = false;
-  explicit DeviceGuard(int dev) {
-    if (hipGetDevice(&prev) == hipSuccess && hipSetDevice(dev) == hipSuccess) ok = true;
-  }
-  ~DeviceGuard() {
-    if (prev >= 0) (void)hipSetDevice(prev);
-  }
-};
-
-// Marks the index busy for the duration of a host call.
-struct BusyGuard {
-  chimera_index *idx;
-  bool ok;
-  explicit BusyGuard(chimera_index *i) : idx(i), ok(i->busy.exchange(1) == 0) {}
-  ~BusyGuard() {
-    if (ok) idx->busy.store(0);
-  }
-};
 
 static int upload(const HostIndex &h, int device, chimera_index **out) {
   int ndev = 0;
@@ -189,19 +169,6 @@ static int check_query_args(const chimera_index *idx, const void *Q, int q_dtype
 
 static const int kMaxK = CHIMERA_MAX_K;
 
-// No C++ exception leaves the C ABI: host allocations inside a call that fail
-// report E_NOMEM.
-template <class F>
-static int guarded(F &&f) {
-  try {
-    return f();
-  } catch (const std::bad_alloc &) {
-    return fail(CHIMERA_E_NOMEM, "host allocation failed");
-  } catch (...) {
-    return fail(CHIMERA_E_INVAL, "internal error");
-  }
-}
-
 // ------------------------------------------------------------- pipeline
 enum Stop { STOP_PROBE = 1, STOP_CANDIDATES = 2, STOP_PRUNE = 3, STOP_FULL = 4, STOP_COLLAB = 5 };
 
@@ -212,6 +179,7 @@ struct Outs {
   int32_t *ids = nullptr; float *scores = nullptr;                               // search
   const CollabOut *collab = nullptr;                                             // collaborative scoring
   bool rabitq = false;                                                           // score from RaBitQ bits
+  const PagesView *pages = nullptr;                                              // score from a paged store
 };
 
 static size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
@@ -229,14 +197,14 @@ struct Carve {
 
 // Exact bytes the sub-batch loop below carves for nb queries.
 static size_t carve_bytes(const chimera_index *idx, int64_t nb, int TQP, int nprobe, int ncand, Stop stop,
-                          bool rq, bool by_doc) {
+                          bool rq, bool by_doc, bool pages) {
   const int64_t rows = nb * TQP;
   const ProbePlan plan = plan_probe(rows, idx->ncent, nprobe);
   size_t b = 0;
   b += align_up((size_t)rows * 128 * 2);                       // Qs
   b += align_up(probe_part_bytes(plan, rows));                 // partial lists
   b += 2 * align_up((size_t)rows * nprobe * 4);                // cent ids / keys
-  if (stop >= STOP_FULL && !rq && !by_doc) b += align_up((size_t)nb * (idx->ncent + 1) * TQP * 4);  // S^T + sentinel rows
+  if (stop >= STOP_FULL && !rq && !by_doc && !pages) b += align_up((size_t)nb * (idx->ncent + 1) * TQP * 4);  // S^T + sentinel rows
   if (by_doc) b += align_up(doc_score_scratch_bytes(nb, TQP, idx->ndocs, ncand, rq));  // visits by document
   if (rq && !by_doc) b += align_up((size_t)rows * RQ_ROW_BYTES) + align_up((size_t)rows * 4);  // query limbs, qsum
   if (stop >= STOP_CANDIDATES) {
@@ -340,7 +308,7 @@ static int run(chimera_index *idx, const void *Q, int q_dtype, int64_t nq, int T
     int64_t lo = 1, hi = std::min<int64_t>(nq, 65535);
     while (lo < hi) {
       const int64_t mid = lo + (hi - lo + 1) / 2;
-      if (carve_bytes(idx, mid, TQP, nprobe, ncand, stop, o.rabitq, docs) <= budget) lo = mid;
+      if (carve_bytes(idx, mid, TQP, nprobe, ncand, stop, o.rabitq, docs, o.pages) <= budget) lo = mid;
       else hi = mid - 1;
     }
     // a launch counts its work-items in 32 bits; the scorer runs about 8 per
@@ -357,22 +325,22 @@ static int run(chimera_index *idx, const void *Q, int q_dtype, int64_t nq, int T
     return doc_score_grouped(b, Tq, nprobe, ncand, idx->ndocs, idx->ntok, idx->nnz, idx->max_doc_len, idx->ncent,
                              idx->ndense, idx->nbits, o.rabitq);
   };
-  bool by_doc = stop == STOP_FULL && (o.rabitq || idx->d_cent16);
+  bool by_doc = stop == STOP_FULL && !o.pages && (o.rabitq || idx->d_cent16);
   int64_t B = largest_for(by_doc);
   if (by_doc && !grouped(B)) {
     by_doc = false;
     B = largest_for(false);
   }
   auto need_for = [&](int64_t b) {
-    size_t n = carve_bytes(idx, b, TQP, nprobe, ncand, stop, o.rabitq, by_doc);
-    if (nq % b) n = std::max(n, carve_bytes(idx, nq % b, TQP, nprobe, ncand, stop, o.rabitq, by_doc));
+    size_t n = carve_bytes(idx, b, TQP, nprobe, ncand, stop, o.rabitq, by_doc, o.pages);
+    if (nq % b) n = std::max(n, carve_bytes(idx, nq % b, TQP, nprobe, ncand, stop, o.rabitq, by_doc, o.pages));
     return n;
   };
   size_t need = need_for(B);
   if (!own) {
     // one query has to fit as it is scored by itself, whatever the batch
     if (by_doc) {
-      const size_t one = carve_bytes(idx, 1, TQP, nprobe, ncand, stop, o.rabitq, false);
+      const size_t one = carve_bytes(idx, 1, TQP, nprobe, ncand, stop, o.rabitq, false, o.pages);
       if (one > fixed.bytes) need = std::max(need, one), B = 1;
     }
     while (need > fixed.bytes && B > 1) need = need_for(--B);
@@ -425,7 +393,7 @@ static int run(chimera_index *idx, const void *Q, int q_dtype, int64_t nq, int T
     uint64_t *part = cv.take<uint64_t>(probe_part_bytes(plan, rows) / 8);
     int32_t *ci = cv.take<int32_t>((size_t)rows * nprobe);
     int32_t *ck = cv.take<int32_t>((size_t)rows * nprobe);
-    float *ST = stop >= STOP_FULL && !o.rabitq && !by_doc ? cv.take<float>((size_t)nb * (idx->ncent + 1) * TQP) : nullptr;
+    float *ST = stop >= STOP_FULL && !o.rabitq && !by_doc && !o.pages ? cv.take<float>((size_t)nb * (idx->ncent + 1) * TQP) : nullptr;
     if (cv.off > scratch_cap) return fail(CHIMERA_E_NOMEM, "internal: scratch plan overflow");
     const size_t qbytes = (size_t)Tq * 128 * (q_dtype == CHIMERA_F32 ? 4 : 2);
     const void *Qb = (const char *)Q + (size_t)q0 * qbytes;
@@ -505,7 +473,9 @@ static int run(chimera_index *idx, const void *Q, int q_dtype, int64_t nq, int T
       continue;
     }
     stage_mark(idx, s, mark);
-    if (o.rabitq && by_doc) {
+    if (o.pages) {
+      launch_pages_score(Qs, CHIMERA_BF16, nb, Tq, TQP, cand, ncand, nval, ncand, *o.pages, fhat, true, s);
+    } else if (o.rabitq && by_doc) {
       char *w = cv.take<char>(doc_score_scratch_bytes(nb, TQP, idx->ndocs, ncand, true));
       if (cv.off > scratch_cap) return fail(CHIMERA_E_NOMEM, "internal: scratch plan overflow");
       launch_doc_score_rq(Qs, nb, Tq, TQP, idx->d_rq_signs, idx->d_doc_off, idx->d_rq_bits, idx->d_rq_g1, idx->ndocs,
@@ -524,6 +494,7 @@ static int run(chimera_index *idx, const void *Q, int q_dtype, int64_t nq, int T
     }
     stage_mark(idx, s, mark);
     launch_topk(fhat, cand, nval, nb, ncand, k, o.ids + q0 * k, o.scores + q0 * k, s);
+    if (o.pages) launch_pages_unscored(o.ids + q0 * k, o.scores + q0 * k, nb * k, s);
     stage_mark(idx, s, mark);
     CHIMERA_HIP(hipGetLastError());
   }
@@ -595,7 +566,7 @@ int chimera_index_delete(chimera_index *idx, const int64_t *doc_ids, int64_t n) 
       return fail(CHIMERA_E_INVAL, "document id %lld (entry %lld) outside [0, %lld)", (long long)doc_ids[i],
                   (long long)i, (long long)idx->ndocs);
   if (n == 0) return CHIMERA_OK;
-  BusyGuard bg(idx);
+  BusyGuard<chimera_index> bg(idx);
   if (!bg.ok) return fail(CHIMERA_E_BUSY, "index in use by another thread");
   DeviceGuard dg(idx->device);
   if (!dg.ok) return fail(CHIMERA_E_DEVICE, "cannot select device %d", idx->device);
@@ -622,7 +593,7 @@ int chimera_index_delete(chimera_index *idx, const int64_t *doc_ids, int64_t n) 
 
 int chimera_index_compact(chimera_index *idx) {
   if (!idx) return fail(CHIMERA_E_INVAL, "null index");
-  BusyGuard bg(idx);
+  BusyGuard<chimera_index> bg(idx);
   if (!bg.ok) return fail(CHIMERA_E_BUSY, "index in use by another thread");
   DeviceGuard dg(idx->device);
   if (!dg.ok) return fail(CHIMERA_E_DEVICE, "cannot select device %d", idx->device);
@@ -741,7 +712,7 @@ int chimera_search(chimera_index *idx, const void *Q, int q_dtype, int64_t nq, i
 // scratch (chimera_search_noalloc).
 static int search_common(chimera_index *idx, const void *Q, int q_dtype, int64_t nq, int32_t Tq, int32_t d,
                          int32_t nprobe, int32_t ncand, int32_t k, int32_t refine, int32_t *ids, float *scores,
-                         void *hip_stream, bool fixed, bool rabitq = false) {
+                         void *hip_stream, bool fixed, bool rabitq = false, const PagesView *pages = nullptr) {
   int rc = check_query_args(idx, Q, q_dtype, nq, Tq, d, nprobe, refine);
   if (rc) return rc;
   if (k < 1) return fail(CHIMERA_E_INVAL, "k must be >= 1");
@@ -751,7 +722,7 @@ static int search_common(chimera_index *idx, const void *Q, int q_dtype, int64_t
   if (nq > 0 && (!ids || !scores)) return fail(CHIMERA_E_INVAL, "null output pointer");
   if (rabitq && !idx->rq) return fail(CHIMERA_E_UNSUPPORTED, "the index holds no RaBitQ codes");
   if (nq == 0) return CHIMERA_OK;
-  BusyGuard bg(idx);
+  BusyGuard<chimera_index> bg(idx);
   if (!bg.ok) return fail(CHIMERA_E_BUSY, "index in use by another thread");
   DeviceGuard dg(idx->device);
   if (!dg.ok) return fail(CHIMERA_E_DEVICE, "cannot select device %d", idx->device);
@@ -767,6 +738,7 @@ static int search_common(chimera_index *idx, const void *Q, int q_dtype, int64_t
   o.ids = ids;
   o.scores = scores;
   o.rabitq = rabitq;
+  o.pages = pages;
   return guarded([&] {
     return run(idx, Q, q_dtype, nq, Tq, nprobe, nc, k, STOP_FULL, o, (hipStream_t)hip_stream, refine, fs);
   });
@@ -790,6 +762,31 @@ int chimera_search_rabitq(chimera_index *idx, const void *Q, int q_dtype, int64_
                        hip_stream, false, true);
 }
 
+int chimera_search_pages(chimera_index *idx, chimera_pages *pg, const void *Q, int q_dtype, int64_t nq, int32_t Tq,
+                         int32_t d, int32_t nprobe, int32_t ncand, int32_t k, int32_t *ids, float *scores,
+                         void *hip_stream) {
+  if (!idx) return fail(CHIMERA_E_INVAL, "null index");
+  if (!pg) return fail(CHIMERA_E_INVAL, "null pages");
+  if (pg->device != idx->device)
+    return fail(CHIMERA_E_INVAL, "the pages are on device %d, the index on device %d", pg->device, idx->device);
+  if (pg->view.ndocs < idx->ndocs)
+    return fail(CHIMERA_E_INVAL, "the pages hold %lld document ids, the index %lld", (long long)pg->view.ndocs,
+                (long long)idx->ndocs);
+  BusyGuard<chimera_pages> bg(pg);
+  if (!bg.ok) return fail(CHIMERA_E_BUSY, "pages in use by another thread");
+  DeviceGuard dg(pg->device);
+  if (!dg.ok) return fail(CHIMERA_E_DEVICE, "cannot select device %d", pg->device);
+  hipStream_t s = (hipStream_t)hip_stream;
+  if (nq > 0)
+    if (int rc = pages_order_before(pg, s)) return rc;
+  int rc = search_common(idx, Q, q_dtype, nq, Tq, d, nprobe, ncand, k, CHIMERA_REFINE_CENTROID, ids, scores, hip_stream,
+                         false, false, &pg->view);
+  // also after an error: some of the search may be queued
+  if (nq > 0)
+    if (int rc2 = pages_order_after(pg, s); rc2 && !rc) rc = rc2;
+  return rc;
+}
+
 static int collab_common(chimera_index *idx, const void *Q, int q_dtype, int64_t nq, int32_t Tq, int32_t d,
                          int32_t nprobe, int32_t ncand, int32_t kfb, int32_t chunks, int32_t k, int32_t *ids,
                          float *scores, int32_t *n_full, int32_t nthreads, void *hip_stream, bool rabitq) {
@@ -803,7 +800,7 @@ static int collab_common(chimera_index *idx, const void *Q, int q_dtype, int64_t
   if (ncand > CHIMERA_MAX_NCAND) return fail(CHIMERA_E_UNSUPPORTED, "ncand %d > %d", ncand, CHIMERA_MAX_NCAND);
   if (nq > 0 && (!ids || !scores || !n_full)) return fail(CHIMERA_E_INVAL, "null output pointer");
   if (nq == 0) return CHIMERA_OK;
-  BusyGuard bg(idx);
+  BusyGuard<chimera_index> bg(idx);
   if (!bg.ok) return fail(CHIMERA_E_BUSY, "index in use by another thread");
   // read under the guard: attach swaps the store while it holds it
   if (rabitq && !idx->rq) return fail(CHIMERA_E_UNSUPPORTED, "the index holds no RaBitQ codes");
@@ -855,7 +852,7 @@ int chimera_probe(chimera_index *idx, const void *Q, int q_dtype, int64_t nq, in
   if (rc) return rc;
   if (nq > 0 && (!cent_ids || !cent_keys)) return fail(CHIMERA_E_INVAL, "null output pointer");
   if (nq == 0) return CHIMERA_OK;
-  BusyGuard bg(idx);
+  BusyGuard<chimera_index> bg(idx);
   if (!bg.ok) return fail(CHIMERA_E_BUSY, "index in use by another thread");
   DeviceGuard dg(idx->device);
   if (!dg.ok) return fail(CHIMERA_E_DEVICE, "cannot select device %d", idx->device);
@@ -872,7 +869,7 @@ int chimera_candidates(chimera_index *idx, const void *Q, int q_dtype, int64_t n
   int rc = check_query_args(idx, Q, q_dtype, nq, Tq, d, nprobe);
   if (rc) return rc;
   if (!offsets || (capacity > 0 && !doc_ids) || capacity < 0) return fail(CHIMERA_E_INVAL, "bad output arguments");
-  BusyGuard bg(idx);
+  BusyGuard<chimera_index> bg(idx);
   if (!bg.ok) return fail(CHIMERA_E_BUSY, "index in use by another thread");
   DeviceGuard dg(idx->device);
   if (!dg.ok) return fail(CHIMERA_E_DEVICE, "cannot select device %d", idx->device);
@@ -905,7 +902,7 @@ int chimera_prune_refine(chimera_index *idx, const void *Q, int q_dtype, int64_t
   if (ncand > CHIMERA_MAX_NCAND) return fail(CHIMERA_E_UNSUPPORTED, "ncand %d > %d", ncand, CHIMERA_MAX_NCAND);
   if (nq > 0 && (!cand_ids || !cand_keys || !n_valid)) return fail(CHIMERA_E_INVAL, "null output pointer");
   if (nq == 0) return CHIMERA_OK;
-  BusyGuard bg(idx);
+  BusyGuard<chimera_index> bg(idx);
   if (!bg.ok) return fail(CHIMERA_E_BUSY, "index in use by another thread");
   DeviceGuard dg(idx->device);
   if (!dg.ok) return fail(CHIMERA_E_DEVICE, "cannot select device %d", idx->device);

@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "../../include/chimera.h"
+#include "pages_book.h"
 
 namespace chimera {
 
@@ -230,6 +231,39 @@ constexpr size_t kFixedScratchBytes = (size_t)CHIMERA_NOALLOC_SCRATCH_MB << 20;
 // kept unused at the array's end, as the grown arena keeps 1/8 spare
 constexpr size_t kFixedScratchGuard = (size_t)1 << 20;
 int fixed_scratch(int device, void **ptr);
+
+// Paged MXFP4 token store (k_pages.hip).  Items, page ids and positions are the
+// plans of pages_book.h; they may lie in host memory that the device can read.
+// X rows of 128 values, ld values apart; out of the read [rows][128].
+constexpr int kPageBytes = 16 * 68;
+struct PagesView {
+  uint8_t *pool = nullptr;   // [npages][kPageBytes]
+  int32_t *table = nullptr;  // [ndocs][stride] page ids
+  int32_t *lens = nullptr;   // [ndocs]
+  int64_t ndocs = 0;
+  int stride = 0;
+};
+void launch_pages_append(const PageItem *items, int64_t nitems, const int32_t *ids, const void *X, int x_dtype,
+                         int64_t ld, uint8_t *pool, int32_t *table, int stride, int32_t *lens, hipStream_t s);
+void launch_pages_read(const PageItem *items, int64_t nitems, const uint8_t *pool, const int32_t *table, int stride,
+                       void *out, int dtype, hipStream_t s);
+void launch_pages_fork(const PageItem *items, int64_t nitems, uint8_t *pool, int32_t *table, int stride, int32_t *lens,
+                       hipStream_t s);
+// in_place: some document is copied onto itself, so the page ids change behind the copy
+void launch_pages_copy(const PageItem *items, int64_t nitems, const int32_t *ids, const int32_t *pos,
+                       const uint8_t *from, const int32_t *from_table, int from_stride, uint8_t *pool, int32_t *table,
+                       int stride, int32_t *lens, bool in_place, hipStream_t s);
+void launch_pages_drop(const int64_t *ids, int64_t n, int32_t *lens, hipStream_t s);
+// MaxSim of Q [nq][q_stride][128] (the first Tq rows of each) with documents ids
+// [nq][ld] (null: 0 .. n - 1), below n_valid [nq] (optional): out [nq][n], float
+// scores or, with keys, int32 keys rint(F * 2^22); Q is bf16 then.
+void launch_pages_score(const void *Q, int q_dtype, int64_t nq, int Tq, int q_stride, const int32_t *ids, int64_t ld,
+                        const int32_t *n_valid, int64_t n, const PagesView &pg, void *out, bool keys, hipStream_t s);
+// Results [n] whose key is the lowest (documents without tokens in the store) become (-1, -inf).
+void launch_pages_unscored(int32_t *ids, float *scores, int64_t n, hipStream_t s);
+// Work on s comes after every earlier call on the store; later calls after the work on s.
+int pages_order_before(chimera_pages *pg, hipStream_t s);
+int pages_order_after(chimera_pages *pg, hipStream_t s);
 
 // Final top-k: ids/scores [nq][k].
 void launch_topk(const int32_t *fhat, const int32_t *cand_ids, const int32_t *n_valid, int64_t nq, int ncand,

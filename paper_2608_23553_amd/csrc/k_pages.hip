@@ -1,0 +1,499 @@
+// k_pages.hip - the paged MXFP4 token store: quantising tokens into pages,
+// reading them back, sharing and copying pages, and the MaxSim of queries with
+// stored documents (Sec. 2.1, Def. 1) straight from the codes.
+//
+// MXFP4 (the OCP microscaling format): a block of 32 values x shares a scale
+// X = 2^(s - 127), s an 8-bit exponent, and holds 32 elements of 4 bits (sign,
+// two exponent bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6).  With E the
+// exponent field of the largest |x| as a float, s = max(E - 2, 0), so the
+// largest element lies in [4, 8) and is 4 or 6 after rounding; elements round
+// to nearest, ties to even, and saturate at 6.  A block with an infinity or a
+// NaN (E = 255) gets s = 255, the format's NaN.
+//
+// A page is 16 tokens, 1088 bytes, in the order in which the matrix
+// instruction takes them (32 x 32 x 64: a lane holds 32 values, one block, of
+// one token): codes [block 4][token 16][16 bytes], then scales
+// [block % 2][token 16][block / 2].  Free slots of a page have the scale 255:
+// their products are NaN, which a maximum passes over, so the scoring has no
+// lengths to compare within a page, and a token with a value that is not
+// finite is never a best match, for the same reason.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "device_common.h"
+#include "internal.h"
+
+namespace chimera {
+
+typedef int v8i32 __attribute__((ext_vector_type(8)));
+typedef unsigned v6u32 __attribute__((ext_vector_type(6)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int CODE_BYTES = 1024;  // of a page; 64 bytes of scales follow
+static_assert(kPageBytes == CODE_BYTES + 64, "16 tokens of 64 + 4 bytes");
+
+// Where block b of a page's token t has its codes and its scale.
+__device__ __forceinline__ int code_at(int b, int t) { return (b * 16 + t) * 16; }
+__device__ __forceinline__ int scale_at(int b, int t) { return CODE_BYTES + ((b & 1) * 16 + t) * 2 + (b >> 1); }
+
+// 2^(s - 127) as a float, s < 255 (s = 0: a subnormal).
+__device__ __forceinline__ float scale_float(uint32_t s) { return __uint_as_float(s ? s << 23 : 0x00400000u); }
+
+// ------------------------------------------------------------ quantising
+// A workgroup takes one item of the plan (up to 16 pages of one document), a
+// wave a page at a time, a lane one block of one token: 32 values, their
+// largest in registers, 16 bytes of codes, one byte of scale.  Bound by memory
+// (256 or 512 bytes read and 68 written a token).
+template <bool F32>
+__global__ __launch_bounds__(256) void k_pages_append(const PageItem *__restrict__ items,
+                                                      const int32_t *__restrict__ ids, const void *__restrict__ X,
+                                                      int64_t ld, uint8_t *__restrict__ pool,
+                                                      int32_t *__restrict__ table, int stride,
+                                                      int32_t *__restrict__ lens) {
+  const PageItem w = items[blockIdx.x];
+  const int lane = lane_id(), t = lane & 15, b = lane >> 4;
+  for (int p = (int)(threadIdx.x >> 6); p < w.npages; p += 4) {
+    const int32_t id = ids[w.pages + p];
+    uint8_t *page = pool + (int64_t)id * kPageBytes;
+    const int i = p * 16 + t - w.fill;  // token of the item; below 0: there before
+    if (i >= 0 && i < w.ntok) {
+      float x[32];
+      if constexpr (F32) {
+        const float4 *src = (const float4 *)((const float *)X + (w.row + i) * ld + b * 32);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const float4 v = src[u];
+          x[4 * u] = v.x, x[4 * u + 1] = v.y, x[4 * u + 2] = v.z, x[4 * u + 3] = v.w;
+        }
+      } else {
+        const uint4 *src = (const uint4 *)((const uint16_t *)X + (w.row + i) * ld + b * 32);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint4 v = src[u];
+          const uint32_t y[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            x[8 * u + 2 * k] = __uint_as_float(y[k] << 16);
+            x[8 * u + 2 * k + 1] = __uint_as_float(y[k] & 0xFFFF0000u);
+          }
+        }
+      }
+      uint32_t top = 0;  // the largest magnitude; as bits, a NaN is larger than any number
+#pragma unroll
+      for (int k = 0; k < 32; ++k) top = max(top, __float_as_uint(x[k]) & 0x7FFFFFFFu);
+      const uint32_t e = top >> 23;
+      const uint32_t s = e == 255 ? 255 : e > 2 ? e - 2 : 0;
+      uint32_t c[4] = {0, 0, 0, 0};
+      if (s != 255) {
+        const float sc = scale_float(s);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          c[u] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c[u], x[8 * u], x[8 * u + 1], sc, 0);
+          c[u] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c[u], x[8 * u + 2], x[8 * u + 3], sc, 1);
+          c[u] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c[u], x[8 * u + 4], x[8 * u + 5], sc, 2);
+          c[u] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c[u], x[8 * u + 6], x[8 * u + 7], sc, 3);
+        }
+      }
+      *(uint4 *)(page + code_at(b, t)) = make_uint4(c[0], c[1], c[2], c[3]);
+      page[scale_at(b, t)] = (uint8_t)s;
+    } else if (i >= w.ntok) {
+      page[scale_at(b, t)] = 255;
+    }
+    if (lane == 0) table[(int64_t)w.doc * stride + w.first + p] = id;
+  }
+  if (threadIdx.x == 0 && w.len >= 0) lens[w.doc] = w.len;
+}
+
+// ------------------------------------------------------------ reading back
+// A lane takes 8 values of a token, so that a wave writes whole rows: 4 rows
+// of bf16 at a time.  Every value (2 significant bits, exponents from -128) is
+// exact in bf16 and in float32.  Bound by memory (68 bytes read, 256 or 512
+// written a token).
+template <bool F32>
+__global__ __launch_bounds__(256) void k_pages_read(const PageItem *__restrict__ items,
+                                                    const uint8_t *__restrict__ pool,
+                                                    const int32_t *__restrict__ table, int stride,
+                                                    void *__restrict__ out) {
+  const PageItem w = items[blockIdx.x];
+  const int lane = lane_id(), seg = lane & 15, b = seg >> 2;
+  for (int p = (int)(threadIdx.x >> 6); p < w.npages; p += 4) {
+    const uint8_t *page = pool + (int64_t)table[(int64_t)w.doc * stride + w.first + p] * kPageBytes;
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+      const int t = it * 4 + (lane >> 4), i = p * 16 + t;
+      if (i >= w.ntok) continue;
+      const uint32_t c = *(const uint32_t *)(page + code_at(b, t) + 4 * (seg & 3));
+      const uint32_t s = page[scale_at(b, t)];
+      const float sc = scale_float(s);
+      f32x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 1),
+                    __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 3)};
+      uint32_t y[8];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        y[2 * k] = s == 255 ? 0x7FC00000u : __float_as_uint(v[k][0]);
+        y[2 * k + 1] = s == 255 ? 0x7FC00000u : __float_as_uint(v[k][1]);
+      }
+      if constexpr (F32) {
+        uint4 *o = (uint4 *)((float *)out + (w.row + i) * CHIMERA_DIM + seg * 8);
+        o[0] = make_uint4(y[0], y[1], y[2], y[3]);
+        o[1] = make_uint4(y[4], y[5], y[6], y[7]);
+      } else {
+        uint4 *o = (uint4 *)((uint16_t *)out + (w.row + i) * CHIMERA_DIM + seg * 8);
+        *o = make_uint4(y[0] >> 16 | y[1], y[2] >> 16 | y[3], y[4] >> 16 | y[5], y[6] >> 16 | y[7]);
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------ sharing and copying
+// A wave a document: its page ids, then the partly filled page behind the
+// shared ones, with free slots behind its ntok tokens.
+__global__ __launch_bounds__(64) void k_pages_fork(const PageItem *__restrict__ items, uint8_t *__restrict__ pool,
+                                                   int32_t *__restrict__ table, int stride,
+                                                   int32_t *__restrict__ lens) {
+  const PageItem w = items[blockIdx.x];
+  const int lane = lane_id(), t = lane & 15, b = lane >> 4;
+  const int32_t *from = table + (int64_t)w.src * stride;
+  int32_t *to = table + (int64_t)w.doc * stride;
+  for (int p = lane; p < w.first; p += 64) to[p] = from[p];
+  if (w.ntok) {
+    const uint8_t *s = pool + (int64_t)from[w.first] * kPageBytes;
+    uint8_t *d = pool + (int64_t)w.pages * kPageBytes;
+    *(uint4 *)(d + code_at(b, t)) = *(const uint4 *)(s + code_at(b, t));
+    d[scale_at(b, t)] = t < w.ntok ? s[scale_at(b, t)] : 255;
+    if (lane == 0) to[w.first] = w.pages;
+  }
+  if (lane == 0) lens[w.doc] = w.len;
+}
+
+// Tokens by position into pages of their own; a lane one block of one token.
+// publish: also the page ids and the length, where no item reads a document
+// that another one writes (else k_pages_publish does, behind it).
+__global__ __launch_bounds__(256) void k_pages_copy(const PageItem *__restrict__ items,
+                                                    const int32_t *__restrict__ ids, const int32_t *__restrict__ pos,
+                                                    const uint8_t *__restrict__ from,
+                                                    const int32_t *__restrict__ from_table, int from_stride,
+                                                    uint8_t *__restrict__ pool, int32_t *__restrict__ table,
+                                                    int stride, int32_t *__restrict__ lens, int publish) {
+  const PageItem w = items[blockIdx.x];
+  const int lane = lane_id(), t = lane & 15, b = lane >> 4;
+  const int32_t *row = from_table + (int64_t)w.src * from_stride;
+  for (int p = (int)(threadIdx.x >> 6); p < w.npages; p += 4) {
+    const int32_t id = ids[w.pages + p];
+    uint8_t *d = pool + (int64_t)id * kPageBytes;
+    const int i = p * 16 + t;
+    if (i < w.ntok) {
+      const int at = pos ? pos[w.row + i] : (int)w.row + i;
+      const uint8_t *s = from + (int64_t)row[at >> 4] * kPageBytes;
+      *(uint4 *)(d + code_at(b, t)) = *(const uint4 *)(s + code_at(b, at & 15));
+      d[scale_at(b, t)] = s[scale_at(b, at & 15)];
+    } else {
+      d[scale_at(b, t)] = 255;
+    }
+    if (publish && lane == 0) table[(int64_t)w.doc * stride + w.first + p] = id;
+  }
+  if (publish && threadIdx.x == 0 && w.len >= 0) lens[w.doc] = w.len;
+}
+
+__global__ __launch_bounds__(64) void k_pages_publish(const PageItem *__restrict__ items,
+                                                      const int32_t *__restrict__ ids, int32_t *__restrict__ table,
+                                                      int stride, int32_t *__restrict__ lens) {
+  const PageItem w = items[blockIdx.x];
+  const int p = (int)threadIdx.x;
+  if (p < w.npages) table[(int64_t)w.doc * stride + w.first + p] = ids[w.pages + p];
+  if (p == 0 && w.len >= 0) lens[w.doc] = w.len;
+}
+
+__global__ __launch_bounds__(256) void k_pages_drop(const int64_t *__restrict__ ids, int64_t n,
+                                                    int32_t *__restrict__ lens) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < n) lens[ids[i]] = 0;
+}
+
+// ------------------------------------------------------------ scoring
+// Operand of the query tokens.  A query token on the grid is an integer
+// k = 2048 q.  It is taken apart into three digits of base 32,
+// k = 1024 d2 + 32 d1 + d0 with |d| <= 16, each of which a 6-bit float of the
+// format e2m3 holds as d / 8 (its values are all the multiples of 1/8 up to 2),
+// so three scaled products of 4-bit documents with 6-bit digits, which run at
+// twice the rate of 8-bit ones, sum up to the exact product with the 16-bit
+// query.  A block of values of 8 or more is shifted right by as many bits as
+// 15 digits' bits lack: an error of at most 2^-15 of the block's largest value.
+// Lane l holds query token l % 32 of a block of 32, dimensions
+// 64 step + 32 (l / 32) .. + 31.
+struct QueryOperand {
+  v6u32 digit[2][3];
+  int scale[2];  // byte j: exponent of digit j
+};
+
+constexpr int OPERAND_WORDS = 2 * 3 * 64 * 6 + 2 * 64;  // of 32 query tokens, in LDS
+
+// All 256 threads: the operands of QB blocks of 32 tokens of one query into
+// LDS, sh [QB][OPERAND_WORDS]; tokens at or past Tq are zero.
+template <int QB, bool F32>
+__device__ __forceinline__ void prepare_query(const void *__restrict__ Q, int Tq, uint32_t *sh) {
+  for (int u = (int)threadIdx.x; u < QB * 128; u += 256) {
+    const int blk = u >> 7, step = (u >> 6) & 1, l = u & 63, j = blk * 32 + (l & 31), d0 = 64 * step + 32 * (l >> 5);
+    float k[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) k[i] = 0.0f;
+    if (j < Tq) {
+      if constexpr (F32) {
+        const float4 *src = (const float4 *)((const float *)Q + (int64_t)j * CHIMERA_DIM + d0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float4 v = src[i];
+          const float y[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int m = 0; m < 4; ++m) k[4 * i + m] = __uint_as_float((uint32_t)grid_bf16_bits(y[m]) << 16) * 2048.0f;
+        }
+      } else {
+        const uint4 *src = (const uint4 *)((const uint16_t *)Q + (int64_t)j * CHIMERA_DIM + d0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint4 v = src[i];
+          const uint32_t y[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int m = 0; m < 4; ++m) {
+            // below 1/16 rounded onto the grid; above it every bf16 is on it
+            k[8 * i + 2 * m] = rintf(__uint_as_float(y[m] << 16) * 2048.0f);
+            k[8 * i + 2 * m + 1] = rintf(__uint_as_float(y[m] & 0xFFFF0000u) * 2048.0f);
+          }
+        }
+      }
+    }
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) top = fmaxf(top, fabsf(k[i]));
+    const int shift = min(max((int)(__float_as_uint(top) >> 23) - 127 - 13, 0), 100);
+    const float down = __uint_as_float((uint32_t)(127 - shift) << 23);
+    f32x16 dig[3][2];  // even and odd dimensions, as the conversion takes them
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const float x = rintf(k[i] * down);
+      const float a2 = rintf(x * (1.0f / 1024.0f)), r = x - 1024.0f * a2, a1 = rintf(r * (1.0f / 32.0f));
+      dig[2][i & 1][i >> 1] = a2;
+      dig[1][i & 1][i >> 1] = a1;
+      dig[0][i & 1][i >> 1] = r - 32.0f * a1;
+    }
+    uint32_t *o = sh + blk * OPERAND_WORDS;
+#pragma unroll
+    for (int m = 0; m < 3; ++m) {
+      const v6u32 c = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(dig[m][0], dig[m][1], 8.0f);
+#pragma unroll
+      for (int i = 0; i < 6; ++i) o[((step * 3 + m) * 64 + l) * 6 + i] = c[i];
+    }
+    // digit m counts 8 * 32^m / 2048 * 2^shift
+    const uint32_t e = (uint32_t)(127 + 3 - 11 + shift);
+    o[2 * 3 * 64 * 6 + step * 64 + l] = e | (e + 5) << 8 | (e + 10) << 16;
+  }
+}
+
+__device__ __forceinline__ void load_query(const uint32_t *sh, QueryOperand &q) {
+  const int l = lane_id();
+#pragma unroll
+  for (int step = 0; step < 2; ++step) {
+#pragma unroll
+    for (int m = 0; m < 3; ++m)
+#pragma unroll
+      for (int i = 0; i < 6; ++i) q.digit[step][m][i] = sh[((step * 3 + m) * 64 + l) * 6 + i];
+    q.scale[step] = (int)sh[2 * 3 * 64 * 6 + step * 64 + l];
+  }
+}
+
+// This lane's part of two pages: the codes of its token's blocks of both steps
+// and their scales (byte = step).
+struct PageOperand {
+  uint4 code[2];
+  int scale;
+};
+// page: of this lane's half of the 32 rows (lanes with bit 4 clear: rows 0 .. 15);
+// negative: no page, every slot free.
+__device__ __forceinline__ PageOperand load_page(const uint8_t *__restrict__ pool, int32_t page) {
+  const int t = lane_id() & 15, h = lane_id() >> 5;
+  PageOperand a;
+  if (page >= 0) {
+    const uint8_t *p = pool + (int64_t)page * kPageBytes;
+    a.code[0] = *(const uint4 *)(p + code_at(h, t));
+    a.code[1] = *(const uint4 *)(p + code_at(h + 2, t));
+    a.scale = *(const uint16_t *)(p + scale_at(h, t));
+  } else {
+    a.code[0] = a.code[1] = make_uint4(0, 0, 0, 0);
+    a.scale = 0xFFFF;
+  }
+  return a;
+}
+
+// <document token, query token> of 32 x 32 pairs: register v of lane l is row
+// 8 (v / 4) + 4 (l / 32) + v % 4, query token l % 32.
+__device__ __forceinline__ f32x16 page_products(const PageOperand &a, const QueryOperand &q) {
+  f32x16 acc = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+#define CHIMERA_MX(STEP, M)                                                                                   \
+  acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(                                                      \
+      v8i32{(int)a.code[STEP].x, (int)a.code[STEP].y, (int)a.code[STEP].z, (int)a.code[STEP].w, 0, 0, 0, 0}, \
+      v8i32{(int)q.digit[STEP][M][0], (int)q.digit[STEP][M][1], (int)q.digit[STEP][M][2],                    \
+            (int)q.digit[STEP][M][3], (int)q.digit[STEP][M][4], (int)q.digit[STEP][M][5], 0, 0},             \
+      acc, 4, 2, STEP, a.scale, M, q.scale[STEP]);
+  // the digits' products in rising order: small sums first
+  CHIMERA_MX(0, 0) CHIMERA_MX(1, 0) CHIMERA_MX(0, 1) CHIMERA_MX(1, 1) CHIMERA_MX(0, 2) CHIMERA_MX(1, 2)
+#undef CHIMERA_MX
+  return acc;
+}
+
+// Key of a score, as the searches rank them: rint(F * 2^22), saturated at the
+// largest floats inside the range, so that the lowest key, -2^31, means
+// -infinity alone.
+__device__ __forceinline__ int32_t score_key(float F) {
+  const float x = rintf(F * KEY_SCALE);
+  return F == -INFINITY ? INT32_MIN : (int32_t)fminf(fmaxf(x, -2147483520.0f), 2147483520.0f);
+}
+
+__global__ __launch_bounds__(256) void k_pages_unscored(int32_t *__restrict__ ids, float *__restrict__ scores,
+                                                        int64_t n) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < n && scores[i] == -512.0f) {  // -2^31 * 2^-22
+    ids[i] = -1;
+    scores[i] = -INFINITY;
+  }
+}
+
+// A workgroup scores documents of one query, four waves dpw entries of its
+// list each; the query's operands are made once in LDS.  Entries: ids
+// [nq][ld] (null: documents 0 .. n - 1), below n_valid[q] where that is given;
+// out [nq][n], float scores or (KEYS) int32 keys.  An entry that names no
+// document, and a document without a finite token, score -infinity.
+template <int QB, bool F32, bool KEYS>
+__global__ __launch_bounds__(256) void k_pages_score(const void *__restrict__ Q, int Tq, int q_stride,
+                                                     const int32_t *__restrict__ ids, int64_t ld,
+                                                     const int32_t *__restrict__ n_valid, int64_t n, int64_t nq,
+                                                     int dpw, const uint8_t *__restrict__ pool,
+                                                     const int32_t *__restrict__ table, int stride,
+                                                     const int32_t *__restrict__ lens, int64_t ndocs,
+                                                     void *__restrict__ out) {
+  __shared__ uint32_t sh[QB * OPERAND_WORDS];
+  const int64_t q = (int64_t)blockIdx.x % nq, chunk = (int64_t)blockIdx.x / nq;
+  const int lane = lane_id();
+  const int64_t last = n_valid ? min(n, (int64_t)n_valid[q]) : n;
+  if (chunk * 4 * dpw >= last) return;  // the whole workgroup
+  prepare_query<QB, F32>((const char *)Q + q * q_stride * (CHIMERA_DIM * (F32 ? 4 : 2)), Tq, sh);
+  __syncthreads();
+  QueryOperand op[QB];
+#pragma unroll
+  for (int u = 0; u < QB; ++u) load_query(sh + u * OPERAND_WORDS, op[u]);
+  const int64_t c0 = (chunk * 4 + (threadIdx.x >> 6)) * dpw, c1 = min(c0 + dpw, last);
+  for (int64_t c = c0; c < c1; ++c) {
+    const int64_t doc = ids ? (int64_t)ids[q * ld + c] : c;
+    const int len = doc >= 0 && doc < ndocs ? lens[doc] : 0;
+    const int npg = (len + 15) >> 4;
+    const int32_t *row = table + doc * stride;
+    float best[QB];
+#pragma unroll
+    for (int u = 0; u < QB; ++u) best[u] = -INFINITY;
+    for (int p = 0; p < npg; p += 2) {
+      const int mine = p + ((lane >> 4) & 1);
+      const PageOperand a = load_page(pool, mine < npg ? row[mine] : -1);
+#pragma unroll
+      for (int u = 0; u < QB; ++u) {
+        const f32x16 s = page_products(a, op[u]);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) best[u] = fmaxf(best[u], s[v]);
+      }
+    }
+    // the other half of the rows, then the sum over query tokens in a fixed
+    // order: 32-bit sums of at most 64 terms
+    float sum = 0.0f;
+#pragma unroll
+    for (int u = 0; u < QB; ++u) {
+      const float m = fmaxf(best[u], shfl_xor(best[u], 32));
+      sum += u * 32 + (lane & 31) < Tq ? m : 0.0f;
+    }
+#pragma unroll
+    for (int m = 16; m >= 1; m >>= 1) sum += shfl_xor(sum, m);
+    if (lane == 0) {
+      if constexpr (KEYS) ((int32_t *)out)[q * n + c] = score_key(sum);
+      else ((float *)out)[q * n + c] = sum;
+    }
+  }
+}
+
+// ------------------------------------------------------------ launchers
+void launch_pages_append(const PageItem *items, int64_t nitems, const int32_t *ids, const void *X, int x_dtype,
+                         int64_t ld, uint8_t *pool, int32_t *table, int stride, int32_t *lens, hipStream_t s) {
+  if (nitems <= 0) return;
+  const dim3 grid((unsigned)nitems);
+  if (x_dtype == CHIMERA_F32)
+    hipLaunchKernelGGL(k_pages_append<true>, grid, dim3(256), 0, s, items, ids, X, ld, pool, table, stride, lens);
+  else
+    hipLaunchKernelGGL(k_pages_append<false>, grid, dim3(256), 0, s, items, ids, X, ld, pool, table, stride, lens);
+}
+
+void launch_pages_read(const PageItem *items, int64_t nitems, const uint8_t *pool, const int32_t *table, int stride,
+                       void *out, int dtype, hipStream_t s) {
+  if (nitems <= 0) return;
+  const dim3 grid((unsigned)nitems);
+  if (dtype == CHIMERA_F32)
+    hipLaunchKernelGGL(k_pages_read<true>, grid, dim3(256), 0, s, items, pool, table, stride, out);
+  else
+    hipLaunchKernelGGL(k_pages_read<false>, grid, dim3(256), 0, s, items, pool, table, stride, out);
+}
+
+void launch_pages_fork(const PageItem *items, int64_t nitems, uint8_t *pool, int32_t *table, int stride, int32_t *lens,
+                       hipStream_t s) {
+  if (nitems <= 0) return;
+  hipLaunchKernelGGL(k_pages_fork, dim3((unsigned)nitems), dim3(64), 0, s, items, pool, table, stride, lens);
+}
+
+void launch_pages_copy(const PageItem *items, int64_t nitems, const int32_t *ids, const int32_t *pos,
+                       const uint8_t *from, const int32_t *from_table, int from_stride, uint8_t *pool, int32_t *table,
+                       int stride, int32_t *lens, bool in_place, hipStream_t s) {
+  if (nitems <= 0) return;
+  const dim3 grid((unsigned)nitems);
+  hipLaunchKernelGGL(k_pages_copy, grid, dim3(256), 0, s, items, ids, pos, from, from_table, from_stride, pool, table,
+                     stride, lens, in_place ? 0 : 1);
+  if (in_place) hipLaunchKernelGGL(k_pages_publish, grid, dim3(64), 0, s, items, ids, table, stride, lens);
+}
+
+void launch_pages_drop(const int64_t *ids, int64_t n, int32_t *lens, hipStream_t s) {
+  if (n <= 0) return;
+  hipLaunchKernelGGL(k_pages_drop, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, ids, n, lens);
+}
+
+void launch_pages_unscored(int32_t *ids, float *scores, int64_t n, hipStream_t s) {
+  if (n <= 0) return;
+  hipLaunchKernelGGL(k_pages_unscored, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, ids, scores, n);
+}
+
+template <int QB>
+static void launch_score_t(const void *Q, int q_dtype, int64_t nq, int Tq, int q_stride, const int32_t *ids,
+                           int64_t ld, const int32_t *n_valid, int64_t n, const PagesView &pg, void *out, bool keys,
+                           hipStream_t s) {
+  const int dpw = (int)std::max<int64_t>(1, std::min<int64_t>(8, n * nq / (4 * 2048)));
+  const int64_t chunks = (n + 4 * dpw - 1) / (4 * dpw);
+  const dim3 grid((unsigned)(chunks * nq));
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, Q, Tq, q_stride, ids, ld, n_valid, n, nq, dpw, pg.pool, pg.table,
+                       pg.stride, pg.lens, pg.ndocs, out);
+  };
+  if (keys) go(k_pages_score<QB, false, true>);
+  else if (q_dtype == CHIMERA_F32) go(k_pages_score<QB, true, false>);
+  else go(k_pages_score<QB, false, false>);
+}
+
+void launch_pages_score(const void *Q, int q_dtype, int64_t nq, int Tq, int q_stride, const int32_t *ids, int64_t ld,
+                        const int32_t *n_valid, int64_t n, const PagesView &pg, void *out, bool keys, hipStream_t s) {
+  if (nq <= 0 || n <= 0) return;
+  // a launch counts its work-items in 32 bits: batches of queries
+  const int64_t per = std::max<int64_t>(1, ((int64_t)1 << 31) / 256 / std::max<int64_t>(1, (n + 3) / 4) / 2);
+  for (int64_t q0 = 0; q0 < nq; q0 += per) {
+    const int64_t nb = std::min(per, nq - q0);
+    const char *Qb = (const char *)Q + (size_t)q0 * q_stride * CHIMERA_DIM * (q_dtype == CHIMERA_F32 ? 4 : 2);
+    const int32_t *idb = ids ? ids + q0 * ld : nullptr;
+    const int32_t *nv = n_valid ? n_valid + q0 : nullptr;
+    char *o = (char *)out + (size_t)q0 * n * 4;
+    if (Tq <= 32) launch_score_t<1>(Qb, q_dtype, nb, Tq, q_stride, idb, ld, nv, n, pg, o, keys, s);
+    else launch_score_t<2>(Qb, q_dtype, nb, Tq, q_stride, idb, ld, nv, n, pg, o, keys, s);
+  }
+}
+
+}  // namespace chimera
