@@ -12,51 +12,6 @@
 
 namespace chimera {
 
-// A call's plan lies in one of a ring of pinned host buffers, which the kernels
-// read directly: a call of one document needs one launch and no copy.  A buffer
-// is free again when the call that used it last has run (its event).
-static int ring_take(chimera_pages *pg, size_t bytes, PagesSlot **out) {
-  PagesSlot &sl = pg->ring[pg->next_slot];
-  if (sl.pending) {
-    CHIMERA_HIP(hipEventSynchronize(sl.done));
-    sl.pending = false;
-  }
-  if (!sl.done) CHIMERA_HIP(hipEventCreateWithFlags(&sl.done, hipEventDisableTiming));
-  if (sl.bytes < bytes) {
-    size_t want = 64 << 10;
-    while (want < bytes) want *= 2;
-    if (sl.host) CHIMERA_HIP(hipHostFree(sl.host));
-    sl.host = nullptr;
-    sl.bytes = 0;
-    hipError_t e = hipHostMalloc((void **)&sl.host, want, hipHostMallocDefault);
-    if (e != hipSuccess) {
-      sl.host = nullptr;
-      (void)hipGetLastError();
-      return hip_fail(e, "plan buffer");
-    }
-    sl.bytes = want;
-  }
-  pg->next_slot = (pg->next_slot + 1) % kPagesRing;
-  *out = &sl;
-  return CHIMERA_OK;
-}
-
-// The stream's work from here on comes after every earlier call on the store.
-int pages_order_before(chimera_pages *pg, hipStream_t s) {
-  if (pg->pending) CHIMERA_HIP(hipStreamWaitEvent(s, pg->done, 0));
-  return CHIMERA_OK;
-}
-int pages_order_after(chimera_pages *pg, hipStream_t s) {
-  CHIMERA_HIP(hipEventRecord(pg->done, s));
-  pg->pending = true;
-  return CHIMERA_OK;
-}
-static int slot_after(PagesSlot *sl, hipStream_t s) {
-  CHIMERA_HIP(hipEventRecord(sl->done, s));
-  sl->pending = true;
-  return CHIMERA_OK;
-}
-
 static bool capturing(hipStream_t s) {
   hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
   if (hipStreamIsCapturing(s, &st) != hipSuccess) {
@@ -64,6 +19,67 @@ static bool capturing(hipStream_t s) {
     return true;  // another stream's capture forbids work on this one
   }
   return st != hipStreamCaptureStatusNone;
+}
+
+int pages_order_before(chimera_pages *pg, hipStream_t s) {
+  if (pg->on_null && s == nullptr) return CHIMERA_OK;
+  if (pg->on_null) {
+    CHIMERA_HIP(hipEventRecord(pg->done, nullptr));
+    pg->pending = true;
+    pg->on_null = false;
+  }
+  if (pg->pending) CHIMERA_HIP(hipStreamWaitEvent(s, pg->done, 0));
+  return CHIMERA_OK;
+}
+int pages_order_after(chimera_pages *pg, hipStream_t s) {
+  pg->on_null = s == nullptr;
+  if (!pg->on_null) {
+    CHIMERA_HIP(hipEventRecord(pg->done, s));
+    pg->pending = true;
+  }
+  return CHIMERA_OK;
+}
+
+static int ring_make(PlanRing &r, size_t half) {
+  for (int i = 0; i < 2; ++i) {
+    if (!r.left[i]) CHIMERA_HIP(hipEventCreateWithFlags(&r.left[i], hipEventDisableTiming));
+    r.pending[i] = false;
+  }
+  if (r.host) CHIMERA_HIP(hipHostFree(r.host));
+  r.host = nullptr;
+  r.half = r.used = 0;
+  r.cur = 0;
+  hipError_t e = hipHostMalloc((void **)&r.host, 2 * half, hipHostMallocDefault);
+  if (e != hipSuccess) {
+    r.host = nullptr;
+    (void)hipGetLastError();
+    return hip_fail(e, "plan buffer");
+  }
+  r.half = half;
+  return CHIMERA_OK;
+}
+
+// Room for a call's plan; s is ordered behind every earlier call (pages_order_before).
+static int ring_take(chimera_pages *pg, size_t bytes, hipStream_t s, char **out) {
+  PlanRing &r = pg->ring;
+  bytes = (bytes + 63) / 64 * 64;
+  if (bytes > r.half) {  // the plans under way lie in the buffer that goes
+    CHIMERA_HIP(hipDeviceSynchronize());
+    size_t half = 512 << 10;
+    while (half < 2 * bytes) half *= 2;
+    if (int rc = ring_make(r, half)) return rc;
+  }
+  if (r.used + bytes > r.half) {
+    CHIMERA_HIP(hipEventRecord(r.left[r.cur], s));
+    r.pending[r.cur] = true;
+    r.cur ^= 1;
+    r.used = 0;
+    if (r.pending[r.cur]) CHIMERA_HIP(hipEventSynchronize(r.left[r.cur]));
+    r.pending[r.cur] = false;
+  }
+  *out = r.host + (size_t)r.cur * r.half + r.used;
+  r.used += bytes;
+  return CHIMERA_OK;
 }
 
 static int book_fail(BookError e, const char *call, const int64_t *ids, int64_t at) {
@@ -139,6 +155,7 @@ int chimera_pages_create(int hip_device, int64_t npages, int64_t ndocs, int32_t 
         }
       }
       CHIMERA_HIP(hipEventCreateWithFlags(&pg->done, hipEventDisableTiming));
+      if (int rc = ring_make(pg->ring, 512 << 10)) return rc;
       CHIMERA_HIP(hipDeviceSynchronize());  // the clears above ran on the null stream
       return CHIMERA_OK;
     });
@@ -160,10 +177,9 @@ void chimera_pages_free(chimera_pages *pg) {
   (void)hipDeviceSynchronize();
   for (void *p : {(void *)pg->view.pool, (void *)pg->view.table, (void *)pg->view.lens})
     if (p) (void)hipFree(p);
-  for (PagesSlot &sl : pg->ring) {
-    if (sl.host) (void)hipHostFree(sl.host);
-    if (sl.done) (void)hipEventDestroy(sl.done);
-  }
+  if (pg->ring.host) (void)hipHostFree(pg->ring.host);
+  for (hipEvent_t e : pg->ring.left)
+    if (e) (void)hipEventDestroy(e);
   if (pg->done) (void)hipEventDestroy(pg->done);
   delete pg;
 }
@@ -216,16 +232,15 @@ int chimera_pages_append(chimera_pages *pg, const int64_t *doc_ids, const int32_
     if (!X) return fail(CHIMERA_E_INVAL, "append: null token pointer");
     if (items > kPagesMaxItems) return fail(CHIMERA_E_UNSUPPORTED, "append: too many tokens in one call");
     if (int rc = check_stream(s, "append")) return rc;
-    PagesSlot *sl = nullptr;
-    if (int rc = ring_take(pg, (size_t)items * sizeof(PageItem) + (size_t)pages * 4, &sl)) return rc;
+    char *plan = nullptr;
     if (int rc = pages_order_before(pg, s)) return rc;
-    PageItem *it = (PageItem *)sl->host;
+    if (int rc = ring_take(pg, (size_t)items * sizeof(PageItem) + (size_t)pages * 4, s, &plan)) return rc;
+    PageItem *it = (PageItem *)plan;
     int32_t *ids = (int32_t *)(it + items);
     pg->book.commit_append(doc_ids, lens, n, doc_stride, it, ids);
     launch_pages_append(it, items, ids, X, x_dtype, ld, pg->view.pool, pg->view.table, pg->view.stride, pg->view.lens,
                         s);
     CHIMERA_HIP(hipGetLastError());
-    if (int rc = slot_after(sl, s)) return rc;
     return pages_order_after(pg, s);
   });
 }
@@ -245,14 +260,13 @@ int chimera_pages_fork(chimera_pages *pg, const int64_t *src_ids, const int64_t 
       return book_fail(e, "fork", dst_ids, at);
     if (n == 0) return CHIMERA_OK;
     if (int rc = check_stream(s, "fork")) return rc;
-    PagesSlot *sl = nullptr;
-    if (int rc = ring_take(pg, (size_t)n * sizeof(PageItem), &sl)) return rc;
+    char *plan = nullptr;
     if (int rc = pages_order_before(pg, s)) return rc;
-    PageItem *it = (PageItem *)sl->host;
+    if (int rc = ring_take(pg, (size_t)n * sizeof(PageItem), s, &plan)) return rc;
+    PageItem *it = (PageItem *)plan;
     pg->book.commit_fork(src_ids, dst_ids, lens, n, it);
     launch_pages_fork(it, n, pg->view.pool, pg->view.table, pg->view.stride, pg->view.lens, s);
     CHIMERA_HIP(hipGetLastError());
-    if (int rc = slot_after(sl, s)) return rc;
     return pages_order_after(pg, s);
   });
 }
@@ -281,19 +295,18 @@ int chimera_pages_copy(chimera_pages *src, const int64_t *src_ids, chimera_pages
     if (items > kPagesMaxItems) return fail(CHIMERA_E_UNSUPPORTED, "copy: too many tokens in one call");
     if (int rc = check_stream(s, "copy")) return rc;
     for (int64_t i = 0; positions && i < n; ++i) npos += lens[i];
-    PagesSlot *sl = nullptr;
-    if (int rc = ring_take(dst, (size_t)items * sizeof(PageItem) + (size_t)(pages + npos) * 4, &sl)) return rc;
+    char *plan = nullptr;
     if (int rc = pages_order_before(dst, s)) return rc;
     if (src != dst)
       if (int rc = pages_order_before(src, s)) return rc;
-    PageItem *it = (PageItem *)sl->host;
+    if (int rc = ring_take(dst, (size_t)items * sizeof(PageItem) + (size_t)(pages + npos) * 4, s, &plan)) return rc;
+    PageItem *it = (PageItem *)plan;
     int32_t *ids = (int32_t *)(it + items), *pos = positions ? ids + pages : nullptr;
     if (npos) std::memcpy(pos, positions, (size_t)npos * 4);
     src->book.commit_copy(src_ids, dst->book, dst_ids, lens, positions, n, it, ids);
     launch_pages_copy(it, items, ids, pos, src->view.pool, src->view.table, src->view.stride, dst->view.pool,
                       dst->view.table, dst->view.stride, dst->view.lens, in_place, s);
     CHIMERA_HIP(hipGetLastError());
-    if (int rc = slot_after(sl, s)) return rc;
     if (src != dst)
       if (int rc = pages_order_after(src, s)) return rc;
     return pages_order_after(dst, s);
@@ -312,10 +325,10 @@ int chimera_pages_drop(chimera_pages *pg, const int64_t *doc_ids, int64_t n, voi
   if (!dg.ok) return fail(CHIMERA_E_DEVICE, "cannot select device %d", pg->device);
   return guarded([&]() -> int {
     if (int rc = check_stream(s, "drop")) return rc;
-    PagesSlot *sl = nullptr;
-    if (int rc = ring_take(pg, (size_t)n * 8, &sl)) return rc;
+    char *plan = nullptr;
     if (int rc = pages_order_before(pg, s)) return rc;
-    int64_t *ids = (int64_t *)sl->host, m = 0;
+    if (int rc = ring_take(pg, (size_t)n * 8, s, &plan)) return rc;
+    int64_t *ids = (int64_t *)plan, m = 0;
     for (int64_t i = 0; i < n; ++i) {
       if (pg->book.len[doc_ids[i]] == 0) continue;  // empty, or named before
       ids[m++] = doc_ids[i];
@@ -324,7 +337,6 @@ int chimera_pages_drop(chimera_pages *pg, const int64_t *doc_ids, int64_t n, voi
     if (m == 0) return CHIMERA_OK;
     launch_pages_drop(ids, m, pg->view.lens, s);
     CHIMERA_HIP(hipGetLastError());
-    if (int rc = slot_after(sl, s)) return rc;
     return pages_order_after(pg, s);
   });
 }
@@ -346,13 +358,12 @@ int chimera_pages_read(chimera_pages *pg, const int64_t *doc_ids, int64_t n, voi
     if (!out) return fail(CHIMERA_E_INVAL, "null output pointer");
     if (items > kPagesMaxItems) return fail(CHIMERA_E_UNSUPPORTED, "read: too many tokens in one call");
     if (int rc = check_stream(s, "read")) return rc;
-    PagesSlot *sl = nullptr;
-    if (int rc = ring_take(pg, (size_t)items * sizeof(PageItem), &sl)) return rc;
+    char *plan = nullptr;
     if (int rc = pages_order_before(pg, s)) return rc;
-    pg->book.plan_read(doc_ids, n, (PageItem *)sl->host);
-    launch_pages_read((PageItem *)sl->host, items, pg->view.pool, pg->view.table, pg->view.stride, out, dtype, s);
+    if (int rc = ring_take(pg, (size_t)items * sizeof(PageItem), s, &plan)) return rc;
+    pg->book.plan_read(doc_ids, n, (PageItem *)plan);
+    launch_pages_read((PageItem *)plan, items, pg->view.pool, pg->view.table, pg->view.stride, out, dtype, s);
     CHIMERA_HIP(hipGetLastError());
-    if (int rc = slot_after(sl, s)) return rc;
     return pages_order_after(pg, s);
   });
 }

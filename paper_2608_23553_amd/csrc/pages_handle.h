@@ -6,14 +6,18 @@
 #include "internal.h"
 
 namespace chimera {
-constexpr int kPagesRing = 16;                    // calls whose plans may be under way
 constexpr int64_t kPagesMaxItems = (1 << 24) - 1;  // work items of a launch (256 threads each, counted in 32 bits)
 
-struct PagesSlot {
-  char *host = nullptr;  // pinned
-  size_t bytes = 0;
-  hipEvent_t done = nullptr;
-  bool pending = false;
+// Pinned host memory that calls' plans lie in, taken from the front to the back
+// of two halves in turn.  Behind the last call of a half an event is recorded;
+// the half is used again once that has passed.
+struct PlanRing {
+  char *host = nullptr;
+  size_t half = 0;  // bytes of each half
+  size_t used = 0;  // of the current half
+  int cur = 0;
+  hipEvent_t left[2] = {nullptr, nullptr};
+  bool pending[2] = {false, false};
 };
 }  // namespace chimera
 
@@ -22,10 +26,12 @@ struct chimera_pages {
   int64_t device_bytes = 0;
   chimera::PageBook book;
   chimera::PagesView view;
-  chimera::PagesSlot ring[chimera::kPagesRing];
-  int next_slot = 0;
-  // the last call's work, which the next call's stream waits for
+  chimera::PlanRing ring;
+  // The last call's work, which a call on another stream waits for: an event on
+  // its stream or, where that was the null stream, none yet.  Work on the null
+  // stream is in order by itself and that stream cannot be destroyed, so the
+  // event (5.7 us of host time, twice a launch) is left until it is needed.
   hipEvent_t done = nullptr;
-  bool pending = false;
+  bool pending = false, on_null = false;
   std::atomic<int> busy{0};
 };
