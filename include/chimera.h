@@ -462,8 +462,9 @@ typedef struct {
 int chimera_pages_create(int hip_device, int64_t npages, int64_t ndocs, int32_t max_len, chimera_pages **out);
 void chimera_pages_free(chimera_pages *pg); /* NULL-safe; waits for pending work */
 int chimera_pages_info_get(const chimera_pages *pg, chimera_pages_info *out);
-/* lens host [n]: the documents' tokens. */
-int chimera_pages_lengths(const chimera_pages *pg, const int64_t *doc_ids, int64_t n, int32_t *lens);
+/* lens host [n]: the documents' tokens; *total their sum.  Either may be NULL. */
+int chimera_pages_lengths(const chimera_pages *pg, const int64_t *doc_ids, int64_t n, int32_t *lens,
+                          int64_t *total);
 
 /* Quantises lens[i] >= 0 tokens to the end of document doc_ids[i] (distinct).
  * X device, rows of d = 128 values (CHIMERA_F32 or CHIMERA_BF16), ld values

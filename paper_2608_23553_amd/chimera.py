@@ -88,7 +88,7 @@ def lib():
         "chimera_pages_create": ([INT, I64, I64, I32, P], INT),
         "chimera_pages_free": ([P], None),
         "chimera_pages_info_get": ([P, P], INT),
-        "chimera_pages_lengths": ([P, P, I64, P], INT),
+        "chimera_pages_lengths": ([P, P, I64, P, P], INT),
         "chimera_pages_append": ([P, P, P, I64, P, INT, I32, I64, I64, P], INT),
         "chimera_pages_fork": ([P, P, P, P, I64, P], INT),
         "chimera_pages_copy": ([P, P, P, P, P, P, I64, P], INT),
@@ -247,10 +247,10 @@ def build_index(centroids_bf16: np.ndarray, nbits: int,
 
 
 # ----------------------------------------------------------------- index
-def _stream_ptr(stream, device=None) -> ctypes.c_void_p:
+def _stream_ptr(stream) -> ctypes.c_void_p:
     import torch
     if stream is None:
-        stream = torch.cuda.current_stream(device)
+        stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream)
 
 
@@ -483,6 +483,8 @@ class Index:
 
 
 # ----------------------------------------------------------------- pages
+# A call on a small store takes microseconds, of which the binding is a part to
+# be seen: what it does for each call is kept short.
 def _aligned(t):
     """t, or a copy where its first value is not 16-byte aligned, as the library asks."""
     return t if t.data_ptr() % 16 == 0 else t.clone()
@@ -496,23 +498,40 @@ def _on(stream):
 
 
 def _ids(ids) -> np.ndarray:
+    if type(ids) is np.ndarray and ids.dtype == np.int64 and ids.ndim == 1 and ids.flags.c_contiguous:
+        return ids
     a = np.asarray(ids)
     if a.dtype != np.int64 and a.size and a.dtype.kind not in "iu":
         raise ValueError(f"document ids must be whole numbers, got {a.dtype}")
-    a = np.ascontiguousarray(a, dtype=np.int64)
-    return a if a.ndim == 1 else a.reshape(-1)
+    return np.ascontiguousarray(a, dtype=np.int64).reshape(-1)
 
 
 def _counts(a, n: int | None, name: str) -> np.ndarray:
     """Lengths or positions as int32 [n]; a value that int32 does not hold is an error, not another value."""
-    b = np.asarray(a)
+    b = a if type(a) is np.ndarray else np.asarray(a)
     if b.dtype != np.int32:
         if b.size and (b.dtype.kind not in "iu" or b.max() > 2**31 - 1 or b.min() < -2**31):
             raise ValueError(f"{name} must be whole numbers of 32 bits")
         b = b.astype(np.int32)
     if b.ndim != 1 or (n is not None and b.shape[0] != n):
         raise ValueError(f"{name} must be [{'n' if n is None else n}], got {list(b.shape)}")
-    return np.ascontiguousarray(b)
+    return b if b.flags.c_contiguous else np.ascontiguousarray(b)
+
+
+_BYTES = ctypes.c_char * 1
+
+
+def _at(a: np.ndarray | None):
+    """A host array's memory as a call takes it."""
+    if a is None:
+        return None
+    # the buffer protocol takes a third of the time of numpy's own attributes
+    return _BYTES.from_buffer(a) if a.size and a.flags.writeable else a.__array_interface__["data"][0]
+
+
+def _total(lens: np.ndarray) -> int:
+    """Sum of lengths, of a few without numpy's reductions, which cost more than they add up."""
+    return sum(lens.tolist()) if lens.size <= 16 else int(lens.sum(dtype=np.int64))
 
 
 class Pages:
@@ -521,10 +540,13 @@ class Pages:
     are host arrays or lists; token vectors, queries and results are device tensors."""
 
     def __init__(self, npages: int, ndocs: int, max_len: int, device: int = 0):
+        import torch
         h = ctypes.c_void_p()
-        _check(lib().chimera_pages_create(device, npages, ndocs, max_len, ctypes.byref(h)))
+        self._lib = lib()
+        _check(self._lib.chimera_pages_create(device, npages, ndocs, max_len, ctypes.byref(h)))
         self._h = h
-        self.ndocs, self.max_len, self.device_index = ndocs, max_len, device
+        self.ndocs, self.max_len, self.device = ndocs, max_len, torch.device("cuda", device)
+        self._types = {torch.float32: F32, torch.bfloat16: BF16}
 
     def close(self):
         if getattr(self, "_h", None) and _lib is not None:
@@ -536,63 +558,60 @@ class Pages:
 
     def info(self) -> dict:
         st = _PagesInfo()
-        _check(lib().chimera_pages_info_get(self._h, ctypes.byref(st)))
+        _check(self._lib.chimera_pages_info_get(self._h, ctypes.byref(st)))
         return _info(st)
 
-    @property
-    def device(self):
+    def _stream(self, stream) -> int:
         import torch
-        return torch.device("cuda", self.device_index)
+        return (torch.cuda.current_stream(self.device) if stream is None else stream).cuda_stream
 
-    def _tensor(self, t, name):
-        """A float32 or bfloat16 tensor on the store's own GPU, and its type for the library."""
-        import torch
-        if not t.is_cuda or t.device.index != self.device_index:
-            raise ValueError(f"{name} is on {t.device}, the pages on cuda:{self.device_index}")
-        if t.dtype == torch.float32:
-            return F32
-        if t.dtype == torch.bfloat16:
-            return BF16
-        raise ValueError(f"{name} must be float32 or bfloat16")
+    def _type(self, t, name) -> int:
+        """The library's name for the type of a tensor on the store's own GPU."""
+        if t.device != self.device:
+            raise ValueError(f"{name} is on {t.device}, the pages on {self.device}")
+        dt = self._types.get(t.dtype)
+        if dt is None:
+            raise ValueError(f"{name} must be float32 or bfloat16")
+        return dt
 
     def lengths(self, ids=None) -> np.ndarray:
         """Tokens of each document of ids (all documents)."""
         a = np.arange(self.ndocs, dtype=np.int64) if ids is None else _ids(ids)
         out = np.empty(a.size, np.int32)
-        _check(lib().chimera_pages_lengths(self._h, a.ctypes.data, a.size, out.ctypes.data))
+        _check(self._lib.chimera_pages_lengths(self._h, _at(a), a.size, _at(out), None))
         return out
 
     def append(self, ids, X, lens=None, stream=None):
         """Quantises tokens to the ends of documents (chimera_pages_append).  X [rows, 128] holds lens[i] rows for each
         document, one behind the other; X [n, L, 128] is a padded batch, of which document i takes the first lens[i]
         rows (lens None: all L)."""
-        dt = self._tensor(X, "X")
+        dt = self._type(X, "X")
         a = _ids(ids)
-        if X.dim() == 3:
-            if X.shape[0] != a.size:
-                raise ValueError(f"X must be [{a.size}, L, 128], got {list(X.shape)}")
-            lens = np.full(a.size, X.shape[1], np.int32) if lens is None else _counts(lens, a.size, "lens")
-            if lens.size and lens.max() > X.shape[1]:
-                raise ValueError(f"lens must be at most {X.shape[1]}, the batch's padded length")
-        elif X.dim() == 2:
+        shape = X.shape
+        if len(shape) == 3:
+            if shape[0] != a.size:
+                raise ValueError(f"X must be [{a.size}, L, 128], got {list(shape)}")
+            lens = np.full(a.size, shape[1], np.int32) if lens is None else _counts(lens, a.size, "lens")
+            if lens.size and lens.max() > shape[1]:
+                raise ValueError(f"lens must be at most {shape[1]}, the batch's padded length")
+        elif len(shape) == 2:
             if lens is None:
                 raise ValueError("lens is needed with X [rows, 128]")
             lens = _counts(lens, a.size, "lens")
-            if int(lens.sum(dtype=np.int64)) != X.shape[0]:
-                raise ValueError(f"lens sum up to {int(lens.sum(dtype=np.int64))}, X has {X.shape[0]} rows")
+            if _total(lens) != shape[0]:
+                raise ValueError(f"lens sum up to {_total(lens)}, X has {shape[0]} rows")
         else:
             raise ValueError("X must be [rows, 128] or [n, L, 128]")
         # rows may be strided, a batch's documents too as long as its rows are evenly spaced
-        unit = 4 if dt == F32 else 8
-        ld = X.stride(-2)
-        doc = X.shape[1] if X.dim() == 3 else 0
-        if (X.stride(-1) != 1 or ld % unit or ld < X.shape[-1] or X.data_ptr() % 16
-                or (X.dim() == 3 and X.shape[0] > 1 and X.stride(0) != X.shape[1] * ld)):
+        steps, doc = X.stride(), shape[1] if len(shape) == 3 else 0
+        ld, x = steps[-2], X.data_ptr()
+        if (steps[-1] != 1 or ld % (4 if dt == F32 else 8) or ld < shape[-1] or x % 16
+                or (doc and shape[0] > 1 and steps[0] != doc * ld)):
             with _on(stream):
                 X = _aligned(X.contiguous())
-            ld = X.shape[-1]
-        _check(lib().chimera_pages_append(self._h, a.ctypes.data, lens.ctypes.data, a.size, X.data_ptr(), dt,
-                                          X.shape[-1], ld, doc, _stream_ptr(stream, self.device_index)))
+            ld, x = shape[-1], X.data_ptr()
+        _check(self._lib.chimera_pages_append(self._h, _at(a), _at(lens), a.size, x, dt, shape[-1], ld, doc,
+                                              self._stream(stream)))
 
     def fork(self, src, dst, lens=None, stream=None):
         """Documents dst (empty) become the first lens[i] tokens (None: all) of documents src, sharing their whole
@@ -601,9 +620,9 @@ class Pages:
         if a.size != b.size:
             raise ValueError(f"{a.size} sources for {b.size} documents")
         lens = None if lens is None else _counts(lens, a.size, "lens")
-        _check(lib().chimera_pages_fork(self._h, a.ctypes.data, b.ctypes.data, _np(lens), a.size, _stream_ptr(stream, self.device_index)))
+        _check(self._lib.chimera_pages_fork(self._h, _at(a), _at(b), _at(lens), a.size, self._stream(stream)))
 
-    def copy(self, src, dst, lens=None, positions=None, to: "Pages" | None = None, stream=None):
+    def copy(self, src, dst, lens=None, positions=None, to: Pages | None = None, stream=None):
         """Documents dst (empty, or the source itself) of `to` (None: this store) become copies, in pages of their own,
         of lens[i] tokens of documents src: the first ones, or those at positions, ascending for each document and one
         document's behind the other's (chimera_pages_copy)."""
@@ -614,56 +633,61 @@ class Pages:
         if positions is not None:
             if lens is None:
                 raise ValueError("lens is needed with positions")
-            positions = _counts(positions, int(lens.sum(dtype=np.int64)), "positions")
-        _check(lib().chimera_pages_copy(self._h, a.ctypes.data, (to or self)._h, b.ctypes.data, _np(lens),
-                                        _np(positions), a.size, _stream_ptr(stream, self.device_index)))
+            positions = _counts(positions, _total(lens), "positions")
+        _check(self._lib.chimera_pages_copy(self._h, _at(a), (to or self)._h, _at(b), _at(lens), _at(positions), a.size,
+                                            self._stream(stream)))
 
     def drop(self, ids, stream=None):
         """Empties documents (chimera_pages_drop)."""
         a = _ids(ids)
-        _check(lib().chimera_pages_drop(self._h, a.ctypes.data, a.size, _stream_ptr(stream, self.device_index)))
+        _check(self._lib.chimera_pages_drop(self._h, _at(a), a.size, self._stream(stream)))
 
     def read(self, ids, dtype=None, out=None, stream=None):
         """The stored values of documents, one behind the other: [sum of lengths, 128], bfloat16 unless dtype says
         float32 (chimera_pages_read)."""
         import torch
         a = _ids(ids)
-        rows = int(self.lengths(a).sum(dtype=np.int64))
+        total = ctypes.c_int64()
+        _check(self._lib.chimera_pages_lengths(self._h, _at(a), a.size, None, ctypes.byref(total)))
+        rows = total.value
         if out is None:
             with _on(stream):
                 out = torch.empty((rows, 128), dtype=dtype or torch.bfloat16, device=self.device)
         elif tuple(out.shape) != (rows, 128) or not out.is_contiguous() or (dtype is not None and out.dtype != dtype):
             raise ValueError(f"out must be a contiguous tensor [{rows}, 128]{'' if dtype is None else f' of {dtype}'}")
-        dt = self._tensor(out, "out")
-        _check(lib().chimera_pages_read(self._h, a.ctypes.data, a.size, out.data_ptr(), dt, _stream_ptr(stream, self.device_index)))
+        _check(self._lib.chimera_pages_read(self._h, _at(a), a.size, out.data_ptr(), self._type(out, "out"),
+                                            self._stream(stream)))
         return out
 
     def score(self, Q, ids=None, out=None, stream=None):
         """Scores float32 [nq, n] of queries Q [nq, Tq, 128] with stored documents (chimera_pages_score): ids int32 on
         the GPU, [nq, n] a list for each query or [n] one for all; None: every document 0 .. ndocs - 1."""
         import torch
-        dt = self._tensor(Q, "Q")
+        dt = self._type(Q, "Q")
         if Q.dim() != 3:
             raise ValueError("Q must be [nq, Tq, d]")
-        with _on(stream):
-            Q = _aligned(Q.contiguous())
         nq, Tq, d = Q.shape
-        n, ld = self.ndocs, 0
+        if not Q.is_contiguous() or Q.data_ptr() % 16:
+            with _on(stream):
+                Q = _aligned(Q.contiguous())
+        n, ld, at = self.ndocs, 0, None
         if ids is not None:
-            if ids.dtype != torch.int32 or ids.device != Q.device or ids.dim() not in (1, 2):
-                raise ValueError(f"ids must be an int32 tensor [n] or [{nq}, n] on {Q.device}")
-            if ids.dim() == 2 and ids.shape[0] != nq:
+            k = ids.dim()
+            if ids.dtype != torch.int32 or ids.device != self.device or k not in (1, 2):
+                raise ValueError(f"ids must be an int32 tensor [n] or [{nq}, n] on {self.device}")
+            if k == 2 and ids.shape[0] != nq:
                 raise ValueError(f"ids must be [{nq}, n], got {list(ids.shape)}")
             n = ids.shape[-1]
-            if ids.stride(-1) != 1 or (ids.dim() == 2 and nq > 1 and ids.stride(0) < n):
+            if ids.stride(-1) != 1 or (k == 2 and nq > 1 and ids.stride(0) < n):
                 with _on(stream):
                     ids = ids.contiguous()
-            ld = ids.stride(0) if ids.dim() == 2 and nq > 1 else 0
+            ld = ids.stride(0) if k == 2 and nq > 1 else 0
+            at = ids.data_ptr()
         if out is None:
             with _on(stream):
-                out = torch.empty((nq, n), dtype=torch.float32, device=Q.device)
-        elif tuple(out.shape) != (nq, n) or out.dtype != torch.float32 or out.device != Q.device or not out.is_contiguous():
-            raise ValueError(f"out must be a contiguous float32 tensor [{nq}, {n}] on {Q.device}")
-        _check(lib().chimera_pages_score(self._h, Q.data_ptr(), dt, nq, Tq, d, None if ids is None else ids.data_ptr(),
-                                         n, ld, out.data_ptr(), _stream_ptr(stream, self.device_index)))
+                out = torch.empty((nq, n), dtype=torch.float32, device=self.device)
+        elif tuple(out.shape) != (nq, n) or out.dtype != torch.float32 or out.device != self.device or not out.is_contiguous():
+            raise ValueError(f"out must be a contiguous float32 tensor [{nq}, {n}] on {self.device}")
+        _check(self._lib.chimera_pages_score(self._h, Q.data_ptr(), dt, nq, Tq, d, at, n, ld, out.data_ptr(),
+                                             self._stream(stream)))
         return out

@@ -229,12 +229,16 @@ struct QueryOperand {
 
 constexpr int OPERAND_WORDS = 2 * 3 * 64 * 6 + 2 * 64;  // of 32 query tokens, in LDS
 
-// All 256 threads: the operands of QB blocks of 32 tokens of one query into
-// LDS, sh [QB][OPERAND_WORDS]; tokens at or past Tq are zero.
-template <int QB, bool F32>
-__device__ __forceinline__ void prepare_query(const void *__restrict__ Q, int Tq, uint32_t *sh) {
-  for (int u = (int)threadIdx.x; u < QB * 128; u += 256) {
-    const int blk = u >> 7, step = (u >> 6) & 1, l = u & 63, j = blk * 32 + (l & 31), d0 = 64 * step + 32 * (l >> 5);
+// All 256 threads: the operands of NB blocks of 32 tokens into LDS, sh
+// [NB][OPERAND_WORDS]: of one query or, PAIR, of one query each (`next` values
+// apart); tokens at or past Tq are zero.
+template <int NB, bool PAIR, bool F32>
+__device__ __forceinline__ void prepare_query(const char *__restrict__ Q0, int64_t next, int Tq, uint32_t *sh) {
+  static_assert(NB <= 2, "a thread a lane of a block's step");
+  if (const int u = (int)threadIdx.x; u < NB * 128) {
+    const int blk = u >> 7, step = (u >> 6) & 1, l = u & 63, d0 = 64 * step + 32 * (l >> 5);
+    const int j = (PAIR ? 0 : blk * 32) + (l & 31);
+    const char *Q = Q0 + (PAIR && blk ? next : 0) * (F32 ? 4 : 2);
     float k[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) k[i] = 0.0f;
@@ -308,25 +312,23 @@ struct PageOperand {
   uint4 code[2];
   int scale;
 };
-// page: of this lane's half of the 32 rows (lanes with bit 4 clear: rows 0 .. 15);
-// negative: no page, every slot free.
-__device__ __forceinline__ PageOperand load_page(const uint8_t *__restrict__ pool, int32_t page) {
-  const int t = lane_id() & 15, h = lane_id() >> 5;
-  PageOperand a;
-  if (page >= 0) {
-    const uint8_t *p = pool + (int64_t)page * kPageBytes;
-    a.code[0] = *(const uint4 *)(p + code_at(h, t));
-    a.code[1] = *(const uint4 *)(p + code_at(h + 2, t));
-    a.scale = *(const uint16_t *)(p + scale_at(h, t));
-  } else {
-    a.code[0] = a.code[1] = make_uint4(0, 0, 0, 0);
-    a.scale = 0xFFFF;
-  }
-  return a;
+// Pages a (rows 0 .. 15, lanes with bit 4 clear) and b (rows 16 .. 31); both
+// false: there is no b, its rows are free slots.
+__device__ __forceinline__ PageOperand load_pages(const uint8_t *__restrict__ pool, int32_t a, int32_t b, bool both) {
+  const int lane = lane_id(), t = lane & 15, h = lane >> 5;
+  const bool second = lane & 16;
+  const uint8_t *p = pool + (int64_t)(second && both ? b : a) * kPageBytes;
+  PageOperand o;
+  o.code[0] = *(const uint4 *)(p + code_at(h, t));
+  o.code[1] = *(const uint4 *)(p + code_at(h + 2, t));
+  o.scale = *(const uint16_t *)(p + scale_at(h, t));
+  if (second && !both) o.scale = 0xFFFF;
+  return o;
 }
 
 // <document token, query token> of 32 x 32 pairs: register v of lane l is row
-// 8 (v / 4) + 4 (l / 32) + v % 4, query token l % 32.
+// 8 (v / 4) + 4 (l / 32) + v % 4, query token l % 32; so v < 8 are the rows of
+// the first page.
 __device__ __forceinline__ f32x16 page_products(const PageOperand &a, const QueryOperand &q) {
   f32x16 acc = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
 #define CHIMERA_MX(STEP, M)                                                                                   \
@@ -358,62 +360,183 @@ __global__ __launch_bounds__(256) void k_pages_unscored(int32_t *__restrict__ id
   }
 }
 
-// A workgroup scores documents of one query, four waves dpw entries of its
-// list each; the query's operands are made once in LDS.  Entries: ids
-// [nq][ld] (null: documents 0 .. n - 1), below n_valid[q] where that is given;
-// out [nq][n], float scores or (KEYS) int32 keys.  An entry that names no
-// document, and a document without a finite token, score -infinity.
-template <int QB, bool F32, bool KEYS>
-__global__ __launch_bounds__(256) void k_pages_score(const void *__restrict__ Q, int Tq, int q_stride,
+// A wave scores list entries one after the other, up to 64 at a time, for NB
+// blocks of 32 query tokens: one query of up to 32 NB tokens or, PAIR, two
+// queries of up to 32 tokens that share the list (each page is loaded once for
+// both).  The entries' pages are strung together: lane j of a window holds the
+// id of its j-th page, a tile is two neighbouring pages whatever documents they
+// belong to, and DEPTH tiles are under way.  A document's maxima over its rows
+// stay in registers until its last page, then go to LDS; every FLUSH documents
+// are summed over the query tokens, 64 / FLUSH lanes each, in the same order
+// whatever NB is.
+constexpr int FLUSH = 16, DEPTH = 4;
+
+#ifndef WPE1
+#define WPE1 3
+#define WPE2 2
+#endif
+template <int NB, bool PAIR, bool F32, bool KEYS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? WPE1 : WPE2))) void k_pages_score(const void *__restrict__ Q, int Tq, int q_stride,
                                                      const int32_t *__restrict__ ids, int64_t ld,
                                                      const int32_t *__restrict__ n_valid, int64_t n, int64_t nq,
-                                                     int dpw, const uint8_t *__restrict__ pool,
+                                                     int dpw, int64_t chunks, const uint8_t *__restrict__ pool,
                                                      const int32_t *__restrict__ table, int stride,
                                                      const int32_t *__restrict__ lens, int64_t ndocs,
                                                      void *__restrict__ out) {
-  __shared__ uint32_t sh[QB * OPERAND_WORDS];
-  const int64_t q = (int64_t)blockIdx.x % nq, chunk = (int64_t)blockIdx.x / nq;
-  const int lane = lane_id();
+  constexpr int PER = PAIR ? 2 : 1;      // queries of a workgroup
+  constexpr int ROW = NB * 32 + 1;       // of the maxima in LDS
+  static_assert(4 * FLUSH * ROW <= NB * OPERAND_WORDS, "the maxima take the operands' place");
+  __shared__ uint32_t sh[NB * OPERAND_WORDS];
+  const int lane = lane_id(), wave = (int)(threadIdx.x >> 6);
+  // Workgroups are dealt to the 8 XCDs in turn.  A chunk of the lists stays with
+  // one XCD, all queries' workgroups for it one behind the other: lists that
+  // ascend name the same documents there, which its L2 then holds.
+  const int64_t groups = (nq + PER - 1) / PER;
+  int64_t chunk, group;
+  if (chunks >= 8) {
+    const int64_t k = blockIdx.x >> 3;
+    chunk = (k / groups) * 8 + (blockIdx.x & 7);
+    group = k % groups;
+  } else {
+    chunk = blockIdx.x / groups;
+    group = blockIdx.x % groups;
+  }
+  const int64_t q = group * PER;
   const int64_t last = n_valid ? min(n, (int64_t)n_valid[q]) : n;
   if (chunk * 4 * dpw >= last) return;  // the whole workgroup
-  prepare_query<QB, F32>((const char *)Q + q * q_stride * (CHIMERA_DIM * (F32 ? 4 : 2)), Tq, sh);
+  const bool two = PAIR && q + 1 < nq;
+  const int64_t step = (int64_t)q_stride * CHIMERA_DIM;
+  prepare_query<NB, PAIR, F32>((const char *)Q + q * step * (F32 ? 4 : 2), two ? step : 0, Tq, sh);
   __syncthreads();
-  QueryOperand op[QB];
+  QueryOperand op[NB];
 #pragma unroll
-  for (int u = 0; u < QB; ++u) load_query(sh + u * OPERAND_WORDS, op[u]);
-  const int64_t c0 = (chunk * 4 + (threadIdx.x >> 6)) * dpw, c1 = min(c0 + dpw, last);
-  for (int64_t c = c0; c < c1; ++c) {
-    const int64_t doc = ids ? (int64_t)ids[q * ld + c] : c;
-    const int len = doc >= 0 && doc < ndocs ? lens[doc] : 0;
-    const int npg = (len + 15) >> 4;
-    const int32_t *row = table + doc * stride;
-    float best[QB];
-#pragma unroll
-    for (int u = 0; u < QB; ++u) best[u] = -INFINITY;
-    for (int p = 0; p < npg; p += 2) {
-      const int mine = p + ((lane >> 4) & 1);
-      const PageOperand a = load_page(pool, mine < npg ? row[mine] : -1);
-#pragma unroll
-      for (int u = 0; u < QB; ++u) {
-        const f32x16 s = page_products(a, op[u]);
-#pragma unroll
-        for (int v = 0; v < 16; ++v) best[u] = fmaxf(best[u], s[v]);
+  for (int u = 0; u < NB; ++u) load_query(sh + u * OPERAND_WORDS, op[u]);
+  __syncthreads();
+  float *best_of = (float *)sh + wave * FLUSH * ROW;
+
+  const int64_t c1 = min((chunk * 4 + wave + 1) * dpw, last);
+  for (int64_t c0 = (chunk * 4 + wave) * dpw; c0 < c1; c0 += 64) {
+    // lane e: entry c0 + e, its document's row of the page table and its pages
+    int64_t row = 0;
+    uint32_t np = 0;
+    if (c0 + lane < c1) {
+      const int64_t doc = ids ? (int64_t)ids[q * ld + c0 + lane] : c0 + lane;
+      if (doc >= 0 && doc < ndocs) {
+        row = doc * stride;
+        np = (uint32_t)(lens[doc] + 15) >> 4;
       }
     }
-    // the other half of the rows, then the sum over query tokens in a fixed
-    // order: 32-bit sums of at most 64 terms
-    float sum = 0.0f;
-#pragma unroll
-    for (int u = 0; u < QB; ++u) {
-      const float m = fmaxf(best[u], shfl_xor(best[u], 32));
-      sum += u * 32 + (lane & 31) < Tq ? m : 0.0f;
+    const uint64_t some = __ballot(np > 0);
+    auto put = [&](int64_t c, int u, float F) {
+      if constexpr (KEYS) ((int32_t *)out)[(q + u) * n + c] = score_key(F);
+      else ((float *)out)[(q + u) * n + c] = F;
+    };
+    if (c0 + lane < c1 && np == 0) {
+      put(c0 + lane, 0, -INFINITY);
+      if (two) put(c0 + lane, 1, -INFINITY);
     }
+    if (some == 0) continue;
+    const uint32_t end = wave_incl_scan(np);
+    const uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)end, 63);
+    row -= (int64_t)(end - np);  // + position in the string of pages
+    // lane r: the r-th entry that has pages
+    const int rank = __builtin_popcountll(some & ((1ull << lane) - 1));
+    const int entry = __builtin_amdgcn_ds_permute((np ? rank : 63 - (lane - rank)) * 4, lane);
+
+    // lane j: the id of page w0 + j of the string, and whether a document ends there
+    auto window = [&](uint32_t w0, uint64_t &ends) -> int32_t {
+      const uint32_t at = w0 + lane;
+      int e = 0;  // entries that end at or before it
 #pragma unroll
-    for (int m = 16; m >= 1; m >>= 1) sum += shfl_xor(sum, m);
-    if (lane == 0) {
-      if constexpr (KEYS) ((int32_t *)out)[q * n + c] = score_key(sum);
-      else ((float *)out)[q * n + c] = sum;
+      for (int step = 32; step >= 1; step >>= 1) {
+        const uint32_t x = (uint32_t)__shfl((int)end, e + step - 1, 64);
+        if (x <= at) e += step;
+      }
+      e = min(e, 63);
+      const int64_t r = ((int64_t)__shfl((int)(row >> 32), e, 64) << 32) | (uint32_t)__shfl((int)(uint32_t)row, e, 64);
+      const uint32_t stop = (uint32_t)__shfl((int)end, e, 64);  // by every lane: lane e may have no page here
+      ends = __ballot(at < total && at + 1 == stop);
+      return at < total ? table[r + at] : 0;
+    };
+
+    float m[NB];
+#pragma unroll
+    for (int u = 0; u < NB; ++u) m[u] = -INFINITY;
+    int slot = 0, flushed = 0;  // documents whose maxima lie in LDS; documents done
+    auto flush = [&]() {
+      __builtin_amdgcn_wave_barrier();
+      const int i = lane / (64 / FLUSH), part = lane % (64 / FLUSH);
+      constexpr int EACH = NB * 32 * FLUSH / 64;  // query tokens of a lane
+      float sum = 0.0f;
+#pragma unroll
+      for (int k = 0; k < EACH; k += 8) {
+        float s8 = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int tok = part * EACH + k + j;
+          const float x = best_of[i * ROW + tok];
+          s8 += (PAIR ? tok & 31 : tok) < Tq ? x : 0.0f;
+        }
+        sum = k ? sum + s8 : s8;
+      }
+      sum += shfl_xor(sum, 1);
+      if constexpr (!PAIR) sum += shfl_xor(sum, 2);
+      const int64_t c = c0 + __shfl(entry, flushed + i, 64);
+      if (i < slot) {
+        if (part == 0) put(c, 0, sum);
+        if (PAIR && part == 2 && two) put(c, 1, sum);
+      }
+      __builtin_amdgcn_wave_barrier();
+      flushed += slot;
+      slot = 0;
+    };
+    auto page_done = [&]() {  // the document's last page: its maxima go to LDS
+#pragma unroll
+      for (int u = 0; u < NB; ++u) {
+        const float x = fmaxf(m[u], shfl_xor(m[u], 32));
+        if (lane < 32) best_of[slot * ROW + u * 32 + lane] = x;
+        m[u] = -INFINITY;
+      }
+      if (++slot == FLUSH) flush();
+    };
+
+    uint64_t ends, next_ends = 0;
+    int32_t page = window(0, ends), next_page = 0;
+    for (uint32_t w0 = 0; w0 < total; w0 += 64) {
+      const int cnt = (int)min(total - w0, 64u), tiles = (cnt + 1) >> 1;
+      if (w0 + 64 < total) next_page = window(w0 + 64, next_ends);
+      auto fetch = [&](int t) {
+        return load_pages(pool, __builtin_amdgcn_readlane(page, 2 * t), __builtin_amdgcn_readlane(page, 2 * t + 1),
+                          2 * t + 1 < cnt);
+      };
+      PageOperand a[DEPTH];
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) a[d] = fetch(min(d, tiles - 1));
+      for (int t0 = 0; t0 < tiles; t0 += DEPTH) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+          const int t = t0 + d;
+          if (t >= tiles) break;
+          f32x16 s[NB];
+#pragma unroll
+          for (int u = 0; u < NB; ++u) s[u] = page_products(a[d], op[u]);
+          a[d] = fetch(min(t + DEPTH, tiles - 1));
+#pragma unroll
+          for (int u = 0; u < NB; ++u)
+#pragma unroll
+            for (int v = 0; v < 8; ++v) m[u] = fmaxf(m[u], s[u][v]);
+          if ((ends >> (2 * t)) & 1) page_done();
+#pragma unroll
+          for (int u = 0; u < NB; ++u)
+#pragma unroll
+            for (int v = 8; v < 16; ++v) m[u] = fmaxf(m[u], s[u][v]);
+          if ((ends >> (2 * t + 1)) & 1) page_done();
+        }
+      }
+      page = next_page;
+      ends = next_ends;
     }
+    if (slot) flush();
   }
 }
 
@@ -464,35 +587,53 @@ void launch_pages_unscored(int32_t *ids, float *scores, int64_t n, hipStream_t s
   hipLaunchKernelGGL(k_pages_unscored, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, ids, scores, n);
 }
 
-template <int QB>
+// List entries of a wave: enough waves to fill the chip first (two rounds of 16
+// a CU), then as many entries as a batch holds.
+static int score_entries(int64_t n, int64_t groups) {
+  static const int most = getenv("PG_MOST") ? atoi(getenv("PG_MOST")) : 64, waves = getenv("PG_WAVES") ? atoi(getenv("PG_WAVES")) : 8192;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(most, n * groups / waves));
+}
+
+template <int NB, bool PAIR>
 static void launch_score_t(const void *Q, int q_dtype, int64_t nq, int Tq, int q_stride, const int32_t *ids,
                            int64_t ld, const int32_t *n_valid, int64_t n, const PagesView &pg, void *out, bool keys,
                            hipStream_t s) {
-  const int dpw = (int)std::max<int64_t>(1, std::min<int64_t>(8, n * nq / (4 * 2048)));
-  const int64_t chunks = (n + 4 * dpw - 1) / (4 * dpw);
-  const dim3 grid((unsigned)(chunks * nq));
+  const int64_t groups = PAIR ? (nq + 1) / 2 : nq;
+  const int dpw = score_entries(n, groups);
+  int64_t chunks = (n + 4 * dpw - 1) / (4 * dpw);
+  if (chunks >= 8) chunks = (chunks + 7) / 8 * 8;
+  const dim3 grid((unsigned)(chunks * groups));
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, Q, Tq, q_stride, ids, ld, n_valid, n, nq, dpw, pg.pool, pg.table,
-                       pg.stride, pg.lens, pg.ndocs, out);
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, Q, Tq, q_stride, ids, ld, n_valid, n, nq, dpw, chunks, pg.pool,
+                       pg.table, pg.stride, pg.lens, pg.ndocs, out);
   };
-  if (keys) go(k_pages_score<QB, false, true>);
-  else if (q_dtype == CHIMERA_F32) go(k_pages_score<QB, true, false>);
-  else go(k_pages_score<QB, false, false>);
+  if constexpr (PAIR) {
+    if (q_dtype == CHIMERA_F32) go(k_pages_score<NB, PAIR, true, false>);
+    else go(k_pages_score<NB, PAIR, false, false>);
+  } else {
+    if (keys) go(k_pages_score<NB, PAIR, false, true>);
+    else if (q_dtype == CHIMERA_F32) go(k_pages_score<NB, PAIR, true, false>);
+    else go(k_pages_score<NB, PAIR, false, false>);
+  }
 }
 
 void launch_pages_score(const void *Q, int q_dtype, int64_t nq, int Tq, int q_stride, const int32_t *ids, int64_t ld,
                         const int32_t *n_valid, int64_t n, const PagesView &pg, void *out, bool keys, hipStream_t s) {
   if (nq <= 0 || n <= 0) return;
-  // a launch counts its work-items in 32 bits: batches of queries
-  const int64_t per = std::max<int64_t>(1, ((int64_t)1 << 31) / 256 / std::max<int64_t>(1, (n + 3) / 4) / 2);
+  const bool pair = Tq <= 32 && nq > 1 && (!ids || ld == 0) && !keys;
+  // a launch counts its work-items in 32 bits: batches of queries, an even number of them
+  const int64_t per_wg = 4 * score_entries(n, nq);
+  const int64_t per = std::max<int64_t>(2, (((int64_t)1 << 31) / 256 / ((n + per_wg - 1) / per_wg + 8)) & ~(int64_t)1);
   for (int64_t q0 = 0; q0 < nq; q0 += per) {
     const int64_t nb = std::min(per, nq - q0);
     const char *Qb = (const char *)Q + (size_t)q0 * q_stride * CHIMERA_DIM * (q_dtype == CHIMERA_F32 ? 4 : 2);
     const int32_t *idb = ids ? ids + q0 * ld : nullptr;
     const int32_t *nv = n_valid ? n_valid + q0 : nullptr;
     char *o = (char *)out + (size_t)q0 * n * 4;
-    if (Tq <= 32) launch_score_t<1>(Qb, q_dtype, nb, Tq, q_stride, idb, ld, nv, n, pg, o, keys, s);
-    else launch_score_t<2>(Qb, q_dtype, nb, Tq, q_stride, idb, ld, nv, n, pg, o, keys, s);
+    auto go = [&](auto launch) { launch(Qb, q_dtype, nb, Tq, q_stride, idb, ld, nv, n, pg, o, keys, s); };
+    if (pair) go(launch_score_t<2, true>);
+    else if (Tq <= 32) go(launch_score_t<1, false>);
+    else go(launch_score_t<2, false>);
   }
 }
 

@@ -196,12 +196,17 @@ int chimera_pages_info_get(const chimera_pages *pg, chimera_pages_info *out) {
   return CHIMERA_OK;
 }
 
-int chimera_pages_lengths(const chimera_pages *pg, const int64_t *doc_ids, int64_t n, int32_t *lens) {
+int chimera_pages_lengths(const chimera_pages *pg, const int64_t *doc_ids, int64_t n, int32_t *lens,
+                          int64_t *total) {
   if (int rc = check_list(pg, doc_ids, n, "lengths")) return rc;
-  if (n > 0 && !lens) return fail(CHIMERA_E_INVAL, "null output pointer");
   for (int64_t i = 0; i < n; ++i)
     if (doc_ids[i] < 0 || doc_ids[i] >= pg->book.ndocs) return book_fail(BookError::id, "lengths", doc_ids, i);
-  for (int64_t i = 0; i < n; ++i) lens[i] = pg->book.len[doc_ids[i]];
+  int64_t sum = 0;
+  for (int64_t i = 0; i < n; ++i) {
+    sum += pg->book.len[doc_ids[i]];
+    if (lens) lens[i] = pg->book.len[doc_ids[i]];
+  }
+  if (total) *total = sum;
   return CHIMERA_OK;
 }
 

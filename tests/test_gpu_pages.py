@@ -149,6 +149,21 @@ def test_scores_of_many_documents(n, nq):
     assert torch.equal(pg.score(Q, lists), torch.gather(got, 1, lists.long()))
 
 
+@pytest.mark.parametrize("pattern", [[0, 6], [0, 0, 17, 0], [6, 0], [0, 40], [5, 6], [16, 0, 16], [1]])
+def test_empty_documents_between_others(pattern):
+    """Lists long enough that a wave takes several entries: one list for many queries, a list each, and one query."""
+    rng = np.random.default_rng(7)
+    pg, docs = _filled(rng, pattern * (1000 // len(pattern)), "bf16")
+    n = len(docs)
+    Q = tensor(units(rng, 41 * 20), "bf16").view(41, 20, 128)
+    got = pg.score(Q)
+    check_scores(got[:1], Q[:1], docs, [range(n)], "one list")
+    assert torch.equal(got, torch.cat([pg.score(q[None]) for q in Q]))
+    lists = torch.arange(n, dtype=torch.int32, device="cuda").repeat(41, 1)
+    assert torch.equal(got, pg.score(Q, lists))
+    assert torch.equal(got.flip(1)[:, 7:], pg.score(Q, lists.flip(1)[:, 7:]))
+
+
 def test_values_that_are_not_finite_never_win():
     rng = np.random.default_rng(8)
     x = units(rng, 5 * 50).reshape(5, 50, 128)

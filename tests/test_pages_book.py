@@ -25,7 +25,7 @@ def test_null_arguments_are_rejected_without_gpu():
     one, len1 = (ctypes.c_int64 * 1)(0), (ctypes.c_int32 * 1)(1)
     assert L.chimera_pages_create(0, 1, 1, 1, None) == bad
     assert L.chimera_pages_info_get(None, None) == bad
-    assert L.chimera_pages_lengths(None, one, 1, len1) == bad
+    assert L.chimera_pages_lengths(None, one, 1, len1, None) == bad
     assert L.chimera_pages_append(None, one, len1, 1, None, 0, 128, 128, 0, None) == bad
     assert L.chimera_pages_fork(None, one, one, len1, 1, None) == bad
     assert L.chimera_pages_copy(None, one, None, one, len1, None, 1, None) == bad
