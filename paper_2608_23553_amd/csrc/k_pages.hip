@@ -212,29 +212,36 @@ __global__ __launch_bounds__(256) void k_pages_drop(const int64_t *__restrict__ 
 }
 
 // ------------------------------------------------------------ scoring
-// Operand of the query tokens.  A query token on the grid is an integer
-// k = 2048 q.  It is taken apart into three digits of base 32,
-// k = 1024 d2 + 32 d1 + d0 with |d| <= 16, each of which a 6-bit float of the
-// format e2m3 holds as d / 8 (its values are all the multiples of 1/8 up to 2),
-// so three scaled products of 4-bit documents with 6-bit digits, which run at
-// twice the rate of 8-bit ones, sum up to the exact product with the 16-bit
-// query.  A block of values of 8 or more is shifted right by as many bits as
-// 15 digits' bits lack: an error of at most 2^-15 of the block's largest value.
-// Lane l holds query token l % 32 of a block of 32, dimensions
+// Operand of the query tokens.  A query value on the grid is an integer
+// k = 2048 q.  The 6-bit floats of the format e2m3 are, times 8, all whole
+// numbers up to 16, the even ones up to 32 and the multiples of 4 up to 60, and
+// their products with 4-bit floats run at twice the rate of 8-bit ones.  Where a
+// block's |k| stay up to 1024 (|q| <= 1/2) two digits of base 32 hold it exactly,
+// k = 32 d1 + d0: up to 512 |d0| <= 16, and above, where bf16 has every fourth k
+// only, d1 is even and d0 a multiple of 4, at most 32.  Larger blocks take three
+// digits |d| <= 16, k = 1024 d2 + 32 d1 + d0; the third one's products are left
+// out for a query that has none.  Blocks of values of 8 or more are shifted right
+// by as many bits as 15 lack: an error of at most 2^-15 of the block's largest
+// value.  Lane l holds query token l % 32 of a block of 32, dimensions
 // 64 step + 32 (l / 32) .. + 31.
 struct QueryOperand {
-  v6u32 digit[2][3];
+  v6u32 digit[2][2];
   int scale[2];  // byte j: exponent of digit j
 };
 
-constexpr int OPERAND_WORDS = 2 * 3 * 64 * 6 + 2 * 64;  // of 32 query tokens, in LDS
+// In LDS, of 32 query tokens: digits 0 and 1 [step][digit][lane][6] (dead once
+// they are in registers), digit 2 [step][lane][6], exponents [step][lane].
+constexpr int LOW_WORDS = 2 * 2 * 64 * 6, HIGH_WORDS = 2 * 64 * 6 + 2 * 64;
 
-// All 256 threads: the operands of NB blocks of 32 tokens into LDS, sh
-// [NB][OPERAND_WORDS]: of one query or, PAIR, of one query each (`next` values
-// apart); tokens at or past Tq are zero.
+// All 256 threads: the operands of NB blocks of 32 tokens into LDS, low [NB]
+// [LOW_WORDS] and high [NB][HIGH_WORDS]: of one query or, PAIR, of one query each
+// (`next` values apart); tokens at or past Tq are zero.  Returns whether this
+// thread's block has a third digit.
 template <int NB, bool PAIR, bool F32>
-__device__ __forceinline__ void prepare_query(const char *__restrict__ Q0, int64_t next, int Tq, uint32_t *sh) {
+__device__ __forceinline__ bool prepare_query(const char *__restrict__ Q0, int64_t next, int Tq, uint32_t *low,
+                                              uint32_t *high) {
   static_assert(NB <= 2, "a thread a lane of a block's step");
+  bool wide = false;
   if (const int u = (int)threadIdx.x; u < NB * 128) {
     const int blk = u >> 7, step = (u >> 6) & 1, l = u & 63, d0 = 64 * step + 32 * (l >> 5);
     const int j = (PAIR ? 0 : blk * 32) + (l & 31);
@@ -272,37 +279,42 @@ __device__ __forceinline__ void prepare_query(const char *__restrict__ Q0, int64
     for (int i = 0; i < 32; ++i) top = fmaxf(top, fabsf(k[i]));
     const int shift = min(max((int)(__float_as_uint(top) >> 23) - 127 - 13, 0), 100);
     const float down = __uint_as_float((uint32_t)(127 - shift) << 23);
+    wide = top > 1024.0f;
     f32x16 dig[3][2];  // even and odd dimensions, as the conversion takes them
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
       const float x = rintf(k[i] * down);
-      const float a2 = rintf(x * (1.0f / 1024.0f)), r = x - 1024.0f * a2, a1 = rintf(r * (1.0f / 32.0f));
+      const float a2 = wide ? rintf(x * (1.0f / 1024.0f)) : 0.0f, r = x - 1024.0f * a2;
+      const float a1 = fabsf(r) > 512.0f ? 2.0f * rintf(r * (1.0f / 64.0f)) : rintf(r * (1.0f / 32.0f));
       dig[2][i & 1][i >> 1] = a2;
       dig[1][i & 1][i >> 1] = a1;
       dig[0][i & 1][i >> 1] = r - 32.0f * a1;
     }
-    uint32_t *o = sh + blk * OPERAND_WORDS;
+    low += blk * LOW_WORDS;
+    high += blk * HIGH_WORDS;
 #pragma unroll
     for (int m = 0; m < 3; ++m) {
       const v6u32 c = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(dig[m][0], dig[m][1], 8.0f);
+      uint32_t *o = m < 2 ? low + ((step * 2 + m) * 64 + l) * 6 : high + (step * 64 + l) * 6;
 #pragma unroll
-      for (int i = 0; i < 6; ++i) o[((step * 3 + m) * 64 + l) * 6 + i] = c[i];
+      for (int i = 0; i < 6; ++i) o[i] = c[i];
     }
     // digit m counts 8 * 32^m / 2048 * 2^shift
     const uint32_t e = (uint32_t)(127 + 3 - 11 + shift);
-    o[2 * 3 * 64 * 6 + step * 64 + l] = e | (e + 5) << 8 | (e + 10) << 16;
+    high[2 * 64 * 6 + step * 64 + l] = e | (e + 5) << 8 | (e + 10) << 16;
   }
+  return wide;
 }
 
-__device__ __forceinline__ void load_query(const uint32_t *sh, QueryOperand &q) {
+__device__ __forceinline__ void load_query(const uint32_t *low, const uint32_t *high, QueryOperand &q) {
   const int l = lane_id();
 #pragma unroll
   for (int step = 0; step < 2; ++step) {
 #pragma unroll
-    for (int m = 0; m < 3; ++m)
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
-      for (int i = 0; i < 6; ++i) q.digit[step][m][i] = sh[((step * 3 + m) * 64 + l) * 6 + i];
-    q.scale[step] = (int)sh[2 * 3 * 64 * 6 + step * 64 + l];
+      for (int i = 0; i < 6; ++i) q.digit[step][m][i] = low[((step * 2 + m) * 64 + l) * 6 + i];
+    q.scale[step] = (int)high[2 * 64 * 6 + step * 64 + l];
   }
 }
 
@@ -312,34 +324,55 @@ struct PageOperand {
   uint4 code[2];
   int scale;
 };
-// Pages a (rows 0 .. 15, lanes with bit 4 clear) and b (rows 16 .. 31); both
-// false: there is no b, its rows are free slots.
-__device__ __forceinline__ PageOperand load_pages(const uint8_t *__restrict__ pool, int32_t a, int32_t b, bool both) {
+// Pages a (rows 0 .. 15, lanes with bit 4 clear) and b (rows 16 .. 31).
+__device__ __forceinline__ PageOperand load_pages(const uint8_t *__restrict__ pool, int32_t a, int32_t b) {
   const int lane = lane_id(), t = lane & 15, h = lane >> 5;
-  const bool second = lane & 16;
-  const uint8_t *p = pool + (int64_t)(second && both ? b : a) * kPageBytes;
+  const uint8_t *p = pool + (int64_t)(lane & 16 ? b : a) * kPageBytes;
   PageOperand o;
   o.code[0] = *(const uint4 *)(p + code_at(h, t));
   o.code[1] = *(const uint4 *)(p + code_at(h + 2, t));
   o.scale = *(const uint16_t *)(p + scale_at(h, t));
-  if (second && !both) o.scale = 0xFFFF;
   return o;
 }
 
 // <document token, query token> of 32 x 32 pairs: register v of lane l is row
 // 8 (v / 4) + 4 (l / 32) + v % 4, query token l % 32; so v < 8 are the rows of
 // the first page.
-__device__ __forceinline__ f32x16 page_products(const PageOperand &a, const QueryOperand &q) {
-  f32x16 acc = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+// The digits in rising order: small sums first.
+__device__ __forceinline__ f32x16 digit_products(const PageOperand &a, const v6u32 (&digit)[2], const int (&scale)[2],
+                                                 f32x16 acc, int m) {
 #define CHIMERA_MX(STEP, M)                                                                                   \
   acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(                                                      \
       v8i32{(int)a.code[STEP].x, (int)a.code[STEP].y, (int)a.code[STEP].z, (int)a.code[STEP].w, 0, 0, 0, 0}, \
-      v8i32{(int)q.digit[STEP][M][0], (int)q.digit[STEP][M][1], (int)q.digit[STEP][M][2],                    \
-            (int)q.digit[STEP][M][3], (int)q.digit[STEP][M][4], (int)q.digit[STEP][M][5], 0, 0},             \
-      acc, 4, 2, STEP, a.scale, M, q.scale[STEP]);
-  // the digits' products in rising order: small sums first
-  CHIMERA_MX(0, 0) CHIMERA_MX(1, 0) CHIMERA_MX(0, 1) CHIMERA_MX(1, 1) CHIMERA_MX(0, 2) CHIMERA_MX(1, 2)
+      v8i32{(int)digit[STEP][0], (int)digit[STEP][1], (int)digit[STEP][2], (int)digit[STEP][3],              \
+            (int)digit[STEP][4], (int)digit[STEP][5], 0, 0},                                                 \
+      acc, 4, 2, STEP, a.scale, M, scale[STEP]);
+  if (m == 0) {
+    CHIMERA_MX(0, 0) CHIMERA_MX(1, 0)
+  } else if (m == 1) {
+    CHIMERA_MX(0, 1) CHIMERA_MX(1, 1)
+  } else {
+    CHIMERA_MX(0, 2) CHIMERA_MX(1, 2)
+  }
 #undef CHIMERA_MX
+  return acc;
+}
+// third: the digit's words of this lane in LDS, or null where there is none.
+__device__ __forceinline__ f32x16 page_products(const PageOperand &a, const QueryOperand &q, const uint32_t *third) {
+  f32x16 acc = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    const v6u32 d[2] = {q.digit[0][m], q.digit[1][m]};
+    acc = digit_products(a, d, q.scale, acc, m);
+  }
+  if (third) {
+    v6u32 d[2];
+#pragma unroll
+    for (int step = 0; step < 2; ++step)
+#pragma unroll
+      for (int i = 0; i < 6; ++i) d[step][i] = third[step * 64 * 6 + i];
+    acc = digit_products(a, d, q.scale, acc, 2);
+  }
   return acc;
 }
 
@@ -366,34 +399,32 @@ __global__ __launch_bounds__(256) void k_pages_unscored(int32_t *__restrict__ id
 // both).  The entries' pages are strung together: lane j of a window holds the
 // id of its j-th page, a tile is two neighbouring pages whatever documents they
 // belong to, and DEPTH tiles are under way.  A document's maxima over its rows
-// stay in registers until its last page, then go to LDS; every FLUSH documents
-// are summed over the query tokens, 64 / FLUSH lanes each, in the same order
+// stay in registers until its last page, then go to a ring in LDS; 16 documents
+// at a time are summed over the query tokens, four lanes each, in the same order
 // whatever NB is.
-constexpr int FLUSH = 16, DEPTH = 4;
+constexpr int DEPTH = 4, FLUSH = 16, RING = 32;
+static_assert(FLUSH + 2 * DEPTH <= RING, "documents that end within DEPTH tiles have room");
 
-#ifndef WPE1
-#define WPE1 3
-#define WPE2 2
-#endif
 template <int NB, bool PAIR, bool F32, bool KEYS>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? WPE1 : WPE2))) void k_pages_score(const void *__restrict__ Q, int Tq, int q_stride,
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4 : 3))) void k_pages_score(const void *__restrict__ Q, int Tq, int q_stride,
                                                      const int32_t *__restrict__ ids, int64_t ld,
                                                      const int32_t *__restrict__ n_valid, int64_t n, int64_t nq,
-                                                     int dpw, int64_t chunks, const uint8_t *__restrict__ pool,
+                                                     int per_wave, int64_t chunks, const uint8_t *__restrict__ pool,
                                                      const int32_t *__restrict__ table, int stride,
                                                      const int32_t *__restrict__ lens, int64_t ndocs,
                                                      void *__restrict__ out) {
   constexpr int PER = PAIR ? 2 : 1;      // queries of a workgroup
   constexpr int ROW = NB * 32 + 1;       // of the maxima in LDS
-  static_assert(4 * FLUSH * ROW <= NB * OPERAND_WORDS, "the maxima take the operands' place");
-  __shared__ uint32_t sh[NB * OPERAND_WORDS];
+  static_assert(4 * RING * ROW >= NB * LOW_WORDS, "the maxima take the first digits' place");
+  __shared__ uint32_t high[NB * HIGH_WORDS], low[4 * RING * ROW];
   const int lane = lane_id(), wave = (int)(threadIdx.x >> 6);
-  // Workgroups are dealt to the 8 XCDs in turn.  A chunk of the lists stays with
-  // one XCD, all queries' workgroups for it one behind the other: lists that
-  // ascend name the same documents there, which its L2 then holds.
+  // Workgroups are dealt to the 8 XCDs in turn.  A chunk of the lists (per_wave
+  // entries for each wave) stays with one XCD, all queries' workgroups for it one
+  // behind the other: lists that ascend name about the same documents there,
+  // some of which its L2 still holds.
   const int64_t groups = (nq + PER - 1) / PER;
   int64_t chunk, group;
-  if (chunks >= 8) {
+  if (chunks % 8 == 0) {
     const int64_t k = blockIdx.x >> 3;
     chunk = (k / groups) * 8 + (blockIdx.x & 7);
     group = k % groups;
@@ -403,124 +434,130 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? W
   }
   const int64_t q = group * PER;
   const int64_t last = n_valid ? min(n, (int64_t)n_valid[q]) : n;
-  if (chunk * 4 * dpw >= last) return;  // the whole workgroup
+  if (chunk * 4 * per_wave >= last) return;  // the whole workgroup
   const bool two = PAIR && q + 1 < nq;
+  const int64_t c0 = (chunk * 4 + wave) * per_wave;
+  // lane e: entry c0 + e, its document's row of the page table and its pages
+  const bool on = lane < per_wave && c0 + lane < last;
+  int64_t row = 0;
+  uint32_t np = 0;
+  if (on) {
+    const int64_t doc = ids ? (int64_t)ids[q * ld + c0 + lane] : c0 + lane;
+    if (doc >= 0 && doc < ndocs) {
+      row = doc * stride;
+      np = (uint32_t)(lens[doc] + 15) >> 4;
+    }
+  }
+  const uint64_t some = __ballot(np > 0);
+  const uint32_t end = wave_incl_scan(np);
+  const uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)end, 63);
+  row -= (int64_t)(end - np);  // + position in the string of pages
+  // lane r: the r-th entry that has pages
+  const int rank = __builtin_popcountll(some & ((1ull << lane) - 1));
+  const int entry = __builtin_amdgcn_ds_permute((np ? rank : 63 - (lane - rank)) * 4, lane);
+
+  // lane j: the id of page w0 + j of the string, and whether a document ends there
+  auto window = [&](uint32_t w0, uint64_t &ends) -> int32_t {
+    const uint32_t at = w0 + lane;
+    int e = 0;  // entries that end at or before it
+#pragma unroll
+    for (int step = 32; step >= 1; step >>= 1) {
+      const uint32_t x = (uint32_t)__shfl((int)end, e + step - 1, 64);
+      if (x <= at) e += step;
+    }
+    e = min(e, 63);
+    const int64_t r = ((int64_t)__shfl((int)(row >> 32), e, 64) << 32) | (uint32_t)__shfl((int)(uint32_t)row, e, 64);
+    const uint32_t stop = (uint32_t)__shfl((int)end, e, 64);  // by every lane: lane e may have no page here
+    ends = __ballot(at < total && at + 1 == stop);
+    return at < total ? table[r + at] : 0;
+  };
+
+  uint64_t ends, next_ends = 0;
+  int32_t page = window(0, ends), next_page = 0;  // under way while the query is prepared
+
   const int64_t step = (int64_t)q_stride * CHIMERA_DIM;
-  prepare_query<NB, PAIR, F32>((const char *)Q + q * step * (F32 ? 4 : 2), two ? step : 0, Tq, sh);
-  __syncthreads();
+  const bool wide = __syncthreads_or(
+      prepare_query<NB, PAIR, F32>((const char *)Q + q * step * (F32 ? 4 : 2), two ? step : 0, Tq, low, high));
   QueryOperand op[NB];
 #pragma unroll
-  for (int u = 0; u < NB; ++u) load_query(sh + u * OPERAND_WORDS, op[u]);
+  for (int u = 0; u < NB; ++u) load_query(low + u * LOW_WORDS, high + u * HIGH_WORDS, op[u]);
   __syncthreads();
-  float *best_of = (float *)sh + wave * FLUSH * ROW;
+  float *best_of = (float *)low + wave * RING * ROW;
 
-  const int64_t c1 = min((chunk * 4 + wave + 1) * dpw, last);
-  for (int64_t c0 = (chunk * 4 + wave) * dpw; c0 < c1; c0 += 64) {
-    // lane e: entry c0 + e, its document's row of the page table and its pages
-    int64_t row = 0;
-    uint32_t np = 0;
-    if (c0 + lane < c1) {
-      const int64_t doc = ids ? (int64_t)ids[q * ld + c0 + lane] : c0 + lane;
-      if (doc >= 0 && doc < ndocs) {
-        row = doc * stride;
-        np = (uint32_t)(lens[doc] + 15) >> 4;
+  auto put = [&](int64_t c, int u, float F) {
+    if constexpr (KEYS) ((int32_t *)out)[(q + u) * n + c] = score_key(F);
+    else ((float *)out)[(q + u) * n + c] = F;
+  };
+  if (on && np == 0) {
+    put(c0 + lane, 0, -INFINITY);
+    if (two) put(c0 + lane, 1, -INFINITY);
+  }
+  if (some == 0) return;
+
+  float m[NB];
+#pragma unroll
+  for (int u = 0; u < NB; ++u) m[u] = -INFINITY;
+  int ended = 0, summed = 0;  // documents whose maxima are, or were, in LDS; those of them that are summed up
+  auto sum_up = [&]() {
+    __builtin_amdgcn_wave_barrier();
+    constexpr int LANES = 64 / FLUSH, EACH = NB * 32 / LANES;  // lanes of a document, query tokens of a lane
+    const int i = summed + lane / LANES, part = lane % LANES;
+    float sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < EACH; k += 8) {
+      float s8 = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int tok = part * EACH + k + j;
+        const float x = best_of[(i % RING) * ROW + tok];
+        s8 += (PAIR ? tok & 31 : tok) < Tq ? x : 0.0f;
       }
+      sum = k ? sum + s8 : s8;
     }
-    const uint64_t some = __ballot(np > 0);
-    auto put = [&](int64_t c, int u, float F) {
-      if constexpr (KEYS) ((int32_t *)out)[(q + u) * n + c] = score_key(F);
-      else ((float *)out)[(q + u) * n + c] = F;
-    };
-    if (c0 + lane < c1 && np == 0) {
-      put(c0 + lane, 0, -INFINITY);
-      if (two) put(c0 + lane, 1, -INFINITY);
+    sum += shfl_xor(sum, 1);
+    if constexpr (!PAIR) sum += shfl_xor(sum, 2);
+    const int64_t c = c0 + __shfl(entry, i & 63, 64);
+    if (i < ended) {
+      if (part == 0) put(c, 0, sum);
+      if (PAIR && part == 2 && two) put(c, 1, sum);
     }
-    if (some == 0) continue;
-    const uint32_t end = wave_incl_scan(np);
-    const uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)end, 63);
-    row -= (int64_t)(end - np);  // + position in the string of pages
-    // lane r: the r-th entry that has pages
-    const int rank = __builtin_popcountll(some & ((1ull << lane) - 1));
-    const int entry = __builtin_amdgcn_ds_permute((np ? rank : 63 - (lane - rank)) * 4, lane);
+    __builtin_amdgcn_wave_barrier();
+    summed = min(summed + FLUSH, ended);
+  };
+  auto page_done = [&]() {  // the document's last page: its maxima go to LDS
+#pragma unroll
+    for (int u = 0; u < NB; ++u) {
+      const float x = fmaxf(m[u], shfl_xor(m[u], 32));
+      if (lane < 32) best_of[(ended % RING) * ROW + u * 32 + lane] = x;
+      m[u] = -INFINITY;
+    }
+    ++ended;
+  };
 
-    // lane j: the id of page w0 + j of the string, and whether a document ends there
-    auto window = [&](uint32_t w0, uint64_t &ends) -> int32_t {
-      const uint32_t at = w0 + lane;
-      int e = 0;  // entries that end at or before it
-#pragma unroll
-      for (int step = 32; step >= 1; step >>= 1) {
-        const uint32_t x = (uint32_t)__shfl((int)end, e + step - 1, 64);
-        if (x <= at) e += step;
-      }
-      e = min(e, 63);
-      const int64_t r = ((int64_t)__shfl((int)(row >> 32), e, 64) << 32) | (uint32_t)__shfl((int)(uint32_t)row, e, 64);
-      const uint32_t stop = (uint32_t)__shfl((int)end, e, 64);  // by every lane: lane e may have no page here
-      ends = __ballot(at < total && at + 1 == stop);
-      return at < total ? table[r + at] : 0;
+  for (uint32_t w0 = 0; w0 < total; w0 += 64) {
+    const int cnt = (int)min(total - w0, 64u), tiles = (cnt + 1) >> 1;
+    if (w0 + 64 < total) next_page = window(w0 + 64, next_ends);
+    // behind the last page its own id stands again
+    auto fetch = [&](int t) {
+      return load_pages(pool, __builtin_amdgcn_readlane(page, min(2 * t, cnt - 1)),
+                        __builtin_amdgcn_readlane(page, min(2 * t + 1, cnt - 1)));
     };
-
-    float m[NB];
+    PageOperand a[DEPTH];
 #pragma unroll
-    for (int u = 0; u < NB; ++u) m[u] = -INFINITY;
-    int slot = 0, flushed = 0;  // documents whose maxima lie in LDS; documents done
-    auto flush = [&]() {
-      __builtin_amdgcn_wave_barrier();
-      const int i = lane / (64 / FLUSH), part = lane % (64 / FLUSH);
-      constexpr int EACH = NB * 32 * FLUSH / 64;  // query tokens of a lane
-      float sum = 0.0f;
+    for (int d = 0; d < DEPTH; ++d) {
+      a[d] = fetch(d);
+      __builtin_amdgcn_sched_barrier(0);  // in this order: the first tile waits for its own loads alone
+    }
+    for (int t0 = 0; t0 < tiles; t0 += DEPTH) {
 #pragma unroll
-      for (int k = 0; k < EACH; k += 8) {
-        float s8 = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int tok = part * EACH + k + j;
-          const float x = best_of[i * ROW + tok];
-          s8 += (PAIR ? tok & 31 : tok) < Tq ? x : 0.0f;
-        }
-        sum = k ? sum + s8 : s8;
-      }
-      sum += shfl_xor(sum, 1);
-      if constexpr (!PAIR) sum += shfl_xor(sum, 2);
-      const int64_t c = c0 + __shfl(entry, flushed + i, 64);
-      if (i < slot) {
-        if (part == 0) put(c, 0, sum);
-        if (PAIR && part == 2 && two) put(c, 1, sum);
-      }
-      __builtin_amdgcn_wave_barrier();
-      flushed += slot;
-      slot = 0;
-    };
-    auto page_done = [&]() {  // the document's last page: its maxima go to LDS
-#pragma unroll
-      for (int u = 0; u < NB; ++u) {
-        const float x = fmaxf(m[u], shfl_xor(m[u], 32));
-        if (lane < 32) best_of[slot * ROW + u * 32 + lane] = x;
-        m[u] = -INFINITY;
-      }
-      if (++slot == FLUSH) flush();
-    };
-
-    uint64_t ends, next_ends = 0;
-    int32_t page = window(0, ends), next_page = 0;
-    for (uint32_t w0 = 0; w0 < total; w0 += 64) {
-      const int cnt = (int)min(total - w0, 64u), tiles = (cnt + 1) >> 1;
-      if (w0 + 64 < total) next_page = window(w0 + 64, next_ends);
-      auto fetch = [&](int t) {
-        return load_pages(pool, __builtin_amdgcn_readlane(page, 2 * t), __builtin_amdgcn_readlane(page, 2 * t + 1),
-                          2 * t + 1 < cnt);
-      };
-      PageOperand a[DEPTH];
-#pragma unroll
-      for (int d = 0; d < DEPTH; ++d) a[d] = fetch(min(d, tiles - 1));
-      for (int t0 = 0; t0 < tiles; t0 += DEPTH) {
-#pragma unroll
-        for (int d = 0; d < DEPTH; ++d) {
-          const int t = t0 + d;
-          if (t >= tiles) break;
+      for (int d = 0; d < DEPTH; ++d) {
+        const int t = t0 + d;
+        if (t < tiles) {
+          // an odd number of pages: the last tile's second half has free slots
+          if (2 * t + 1 == cnt && (lane & 16)) a[d].scale = 0xFFFF;
           f32x16 s[NB];
 #pragma unroll
-          for (int u = 0; u < NB; ++u) s[u] = page_products(a[d], op[u]);
-          a[d] = fetch(min(t + DEPTH, tiles - 1));
+          for (int u = 0; u < NB; ++u) s[u] = page_products(a[d], op[u], wide ? high + u * HIGH_WORDS + lane * 6 : nullptr);
 #pragma unroll
           for (int u = 0; u < NB; ++u)
 #pragma unroll
@@ -532,12 +569,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? W
             for (int v = 8; v < 16; ++v) m[u] = fmaxf(m[u], s[u][v]);
           if ((ends >> (2 * t + 1)) & 1) page_done();
         }
+        // behind the branch, so that the registers of a tile stay where they are
+        a[d] = fetch(t + DEPTH);
       }
-      page = next_page;
-      ends = next_ends;
+      if (ended - summed >= FLUSH) sum_up();
     }
-    if (slot) flush();
+    page = next_page;
+    ends = next_ends;
   }
+  while (summed < ended) sum_up();
 }
 
 // ------------------------------------------------------------ launchers
@@ -587,11 +627,14 @@ void launch_pages_unscored(int32_t *ids, float *scores, int64_t n, hipStream_t s
   hipLaunchKernelGGL(k_pages_unscored, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, ids, scores, n);
 }
 
-// List entries of a wave: enough waves to fill the chip first (two rounds of 16
-// a CU), then as many entries as a batch holds.
-static int score_entries(int64_t n, int64_t groups) {
-  static const int most = getenv("PG_MOST") ? atoi(getenv("PG_MOST")) : 64, waves = getenv("PG_WAVES") ? atoi(getenv("PG_WAVES")) : 8192;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(most, n * groups / waves));
+// List entries of a wave: enough waves to fill the chip first (16 a CU), then as
+// many entries as a wave can take (64) where all queries share the list, 16 where
+// each has its own: short chunks keep more of what the queries of a chunk read in
+// an XCD's L2 (256 x 2048 entries of 50,000 documents: 262, 252, 286 and 320 us
+// with 8, 16, 32 and 64 entries; 64 queries x 30,000 documents: 612, 550, 519 and
+// 516 us).
+static int score_entries(int64_t n, int64_t groups, bool shared) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>(shared ? 64 : 16, n * groups / 4096));
 }
 
 template <int NB, bool PAIR>
@@ -599,12 +642,12 @@ static void launch_score_t(const void *Q, int q_dtype, int64_t nq, int Tq, int q
                            int64_t ld, const int32_t *n_valid, int64_t n, const PagesView &pg, void *out, bool keys,
                            hipStream_t s) {
   const int64_t groups = PAIR ? (nq + 1) / 2 : nq;
-  const int dpw = score_entries(n, groups);
-  int64_t chunks = (n + 4 * dpw - 1) / (4 * dpw);
+  const int per_wave = score_entries(n, groups, !ids || ld == 0);
+  int64_t chunks = (n + 4 * per_wave - 1) / (4 * per_wave);
   if (chunks >= 8) chunks = (chunks + 7) / 8 * 8;
   const dim3 grid((unsigned)(chunks * groups));
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, Q, Tq, q_stride, ids, ld, n_valid, n, nq, dpw, chunks, pg.pool,
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, Q, Tq, q_stride, ids, ld, n_valid, n, nq, per_wave, chunks, pg.pool,
                        pg.table, pg.stride, pg.lens, pg.ndocs, out);
   };
   if constexpr (PAIR) {
@@ -621,9 +664,9 @@ void launch_pages_score(const void *Q, int q_dtype, int64_t nq, int Tq, int q_st
                         const int32_t *n_valid, int64_t n, const PagesView &pg, void *out, bool keys, hipStream_t s) {
   if (nq <= 0 || n <= 0) return;
   const bool pair = Tq <= 32 && nq > 1 && (!ids || ld == 0) && !keys;
-  // a launch counts its work-items in 32 bits: batches of queries, an even number of them
-  const int64_t per_wg = 4 * score_entries(n, nq);
-  const int64_t per = std::max<int64_t>(2, (((int64_t)1 << 31) / 256 / ((n + per_wg - 1) / per_wg + 8)) & ~(int64_t)1);
+  // a launch counts its work-items in 32 bits: queries in batches of an even number
+  const int64_t few = std::max<int64_t>(1, n / 64 + 8);  // workgroups of a query where there are more than 4096 waves
+  const int64_t per = std::max<int64_t>(2, (((int64_t)1 << 23) / few) & ~(int64_t)1);
   for (int64_t q0 = 0; q0 < nq; q0 += per) {
     const int64_t nb = std::min(per, nq - q0);
     const char *Qb = (const char *)Q + (size_t)q0 * q_stride * CHIMERA_DIM * (q_dtype == CHIMERA_F32 ? 4 : 2);

@@ -181,7 +181,7 @@ def test_values_that_are_not_finite_never_win():
     assert got[0, 1] == -np.inf and torch.isfinite(got[0, [0, 2, 3, 4]]).all()
 
 
-@pytest.mark.parametrize("scale", [2.0**-12, 0.01, 1.0, 3.0, 7.9, 8.1, 1000.0, 1e30])
+@pytest.mark.parametrize("scale", [2.0**-12, 0.01, 0.24, 0.26, 0.499, 0.502, 1.0, 3.0, 7.9, 8.1, 1000.0, 1e30])
 def test_queries_and_documents_of_any_size(scale):
     """Query values below and above 8, and documents scaled the other way."""
     rng = np.random.default_rng(9)
@@ -193,6 +193,26 @@ def test_queries_and_documents_of_any_size(scale):
     Q = tensor(rng.uniform(-1, 1, (2 * 7, 128)) * scale).view(2, 7, 128)
     docs = [v[:10], v[10:30], v[30:]]
     check_scores(pg.score(Q), Q, docs, [range(3)] * 2, f"scale {scale}")
+
+
+def test_every_query_value_below_a_half_and_some_above():
+    """One-hot documents of value 1: the score is the query value itself, exactly, in blocks whose largest value is up
+    to 1/2 and beyond (two digits and three)."""
+    k = np.arange(0, 4096, dtype=np.float64) / 2048
+    bf = torch.from_numpy(k).to(torch.bfloat16).double().numpy()
+    k = k[(k < 0.0625) | (k == bf)]                    # the grid
+    k = np.concatenate([k, -k])
+    eye = np.zeros((128, 128), np.float32)
+    eye[np.arange(128), np.arange(128)] = 1
+    X = tensor(eye)
+    pg = Pages(128, 128, 1)
+    pg.append(np.arange(128), X, [1] * 128)
+    for most in (0.25, 0.5, 2.0):
+        v = k[np.abs(k) <= most]
+        v = np.resize(v, -(-len(v) // 128) * 128).reshape(-1, 1, 128)
+        for order in (v, np.random.default_rng(0).permuted(v.reshape(-1)).reshape(v.shape)):
+            got = pg.score(torch.from_numpy(order).float().cuda())
+            assert np.array_equal(got.cpu().numpy(), order[:, 0]), most
 
 
 def test_unit_vectors_score_to_the_last_bit():
