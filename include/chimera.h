@@ -452,13 +452,13 @@ typedef struct {
   int64_t free_pages;   /* pages that no document holds */
   int64_t ndocs;        /* document ids */
   int64_t ntokens;      /* tokens of all documents (shared ones counted for each) */
-  int64_t device_bytes; /* device memory of the store: 1088 npages + 4 ndocs (1 + ceil(max_len / 16)) */
+  int64_t device_bytes; /* device memory of the store: 1088 npages + 4 ndocs (1 + 8 ceil(max_len / 128)) */
   int32_t max_len;      /* tokens a document can have */
   int32_t device;       /* HIP device ordinal */
 } chimera_pages_info;
 
 /* npages, ndocs 1 .. 2^31 - 1, max_len 1 .. CHIMERA_PAGES_MAX_LEN.  Host memory:
- * 8 npages + 4 ndocs (2 + ceil(max_len / 16)) bytes. */
+ * 8 npages + 8 ndocs (1 + 4 ceil(max_len / 128)) bytes. */
 int chimera_pages_create(int hip_device, int64_t npages, int64_t ndocs, int32_t max_len, chimera_pages **out);
 void chimera_pages_free(chimera_pages *pg); /* NULL-safe; waits for pending work */
 int chimera_pages_info_get(const chimera_pages *pg, chimera_pages_info *out);

@@ -243,14 +243,17 @@ struct PagesView {
   int64_t ndocs = 0;
   int stride = 0;
 };
+// bytes (a multiple of 16) of host memory to the device
+void launch_pages_plan(const void *host, void *dev, size_t bytes, hipStream_t s);
 void launch_pages_append(const PageItem *items, int64_t nitems, const int32_t *ids, const void *X, int x_dtype,
                          int64_t ld, uint8_t *pool, int32_t *table, int stride, int32_t *lens, hipStream_t s);
 void launch_pages_read(const PageItem *items, int64_t nitems, const uint8_t *pool, const int32_t *table, int stride,
                        void *out, int dtype, hipStream_t s);
 void launch_pages_fork(const PageItem *items, int64_t nitems, uint8_t *pool, int32_t *table, int stride, int32_t *lens,
                        hipStream_t s);
-// in_place: some document is copied onto itself, so the page ids change behind the copy
-void launch_pages_copy(const PageItem *items, int64_t nitems, const int32_t *ids, const int32_t *pos,
+// pos: int32 or, short_pos, uint16 positions; in_place: some document is copied
+// onto itself, so the page ids change behind the copy
+void launch_pages_copy(const PageItem *items, int64_t nitems, const int32_t *ids, const void *pos, bool short_pos,
                        const uint8_t *from, const int32_t *from_table, int from_stride, uint8_t *pool, int32_t *table,
                        int stride, int32_t *lens, bool in_place, hipStream_t s);
 void launch_pages_drop(const int64_t *ids, int64_t n, int32_t *lens, hipStream_t s);

@@ -40,6 +40,21 @@ __device__ __forceinline__ int scale_at(int b, int t) { return CODE_BYTES + ((b 
 // 2^(s - 127) as a float, s < 255 (s = 0: a subnormal).
 __device__ __forceinline__ float scale_float(uint32_t s) { return __uint_as_float(s ? s << 23 : 0x00400000u); }
 
+// ------------------------------------------------------------ plans
+// A plan on its way from host memory: whole lines in order, which the bus takes
+// at 38 GB/s, where items read one a wave come at 14.
+__global__ __launch_bounds__(256) void k_pages_plan(const uint4 *__restrict__ host, uint4 *__restrict__ dev,
+                                                    int64_t n) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < n) dev[i] = host[i];
+}
+
+void launch_pages_plan(const void *host, void *dev, size_t bytes, hipStream_t s) {
+  const int64_t n = (int64_t)(bytes / 16);
+  hipLaunchKernelGGL(k_pages_plan, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, (const uint4 *)host,
+                     (uint4 *)dev, n);
+}
+
 // ------------------------------------------------------------ quantising
 // A workgroup takes one item of the plan (up to 16 pages of one document), a
 // wave a page at a time, a lane one block of one token: 32 values, their
@@ -170,8 +185,9 @@ __global__ __launch_bounds__(64) void k_pages_fork(const PageItem *__restrict__ 
 // Tokens by position into pages of their own; a lane one block of one token.
 // publish: also the page ids and the length, where no item reads a document
 // that another one writes (else k_pages_publish does, behind it).
+template <class Pos>
 __global__ __launch_bounds__(256) void k_pages_copy(const PageItem *__restrict__ items,
-                                                    const int32_t *__restrict__ ids, const int32_t *__restrict__ pos,
+                                                    const int32_t *__restrict__ ids, const Pos *__restrict__ pos,
                                                     const uint8_t *__restrict__ from,
                                                     const int32_t *__restrict__ from_table, int from_stride,
                                                     uint8_t *__restrict__ pool, int32_t *__restrict__ table,
@@ -184,7 +200,7 @@ __global__ __launch_bounds__(256) void k_pages_copy(const PageItem *__restrict__
     uint8_t *d = pool + (int64_t)id * kPageBytes;
     const int i = p * 16 + t;
     if (i < w.ntok) {
-      const int at = pos ? pos[w.row + i] : (int)w.row + i;
+      const int at = pos ? (int)pos[w.row + i] : (int)w.row + i;
       const uint8_t *s = from + (int64_t)row[at >> 4] * kPageBytes;
       *(uint4 *)(d + code_at(b, t)) = *(const uint4 *)(s + code_at(b, at & 15));
       d[scale_at(b, t)] = s[scale_at(b, at & 15)];
@@ -607,13 +623,18 @@ void launch_pages_fork(const PageItem *items, int64_t nitems, uint8_t *pool, int
   hipLaunchKernelGGL(k_pages_fork, dim3((unsigned)nitems), dim3(64), 0, s, items, pool, table, stride, lens);
 }
 
-void launch_pages_copy(const PageItem *items, int64_t nitems, const int32_t *ids, const int32_t *pos,
+void launch_pages_copy(const PageItem *items, int64_t nitems, const int32_t *ids, const void *pos, bool short_pos,
                        const uint8_t *from, const int32_t *from_table, int from_stride, uint8_t *pool, int32_t *table,
                        int stride, int32_t *lens, bool in_place, hipStream_t s) {
   if (nitems <= 0) return;
   const dim3 grid((unsigned)nitems);
-  hipLaunchKernelGGL(k_pages_copy, grid, dim3(256), 0, s, items, ids, pos, from, from_table, from_stride, pool, table,
-                     stride, lens, in_place ? 0 : 1);
+  const int publish = in_place ? 0 : 1;
+  if (short_pos)
+    hipLaunchKernelGGL(k_pages_copy<uint16_t>, grid, dim3(256), 0, s, items, ids, (const uint16_t *)pos, from,
+                       from_table, from_stride, pool, table, stride, lens, publish);
+  else
+    hipLaunchKernelGGL(k_pages_copy<int32_t>, grid, dim3(256), 0, s, items, ids, (const int32_t *)pos, from,
+                       from_table, from_stride, pool, table, stride, lens, publish);
   if (in_place) hipLaunchKernelGGL(k_pages_publish, grid, dim3(64), 0, s, items, ids, table, stride, lens);
 }
 

@@ -9,6 +9,7 @@
 #pragma once
 
 #include <cstdint>
+#include <cstring>
 #include <vector>
 
 namespace chimera {
@@ -22,14 +23,15 @@ constexpr int kItemPages = 16;
 struct PageItem {
   int32_t doc = 0;      // document written (read: document read)
   int32_t first = 0;    // its first page here, as a page of the document
-  int32_t npages = 0;
   int32_t pages = 0;    // position of their page ids in the plan's list
-  int32_t fill = 0;     // tokens that the first page holds already
-  int32_t ntok = 0;     // tokens to write (read) from there
   int32_t len = -1;     // the document's length after the call; -1: another item sets it
-  int32_t src = 0;      // copy, fork: the document read
   int64_t row = 0;      // append, read: first row of the tensor; copy: first position in the plan's list, or first token
+  int32_t src = 0;      // copy, fork: the document read
+  uint16_t ntok = 0;    // tokens to write (read) from there
+  uint8_t npages = 0;
+  uint8_t fill = 0;     // tokens that the first page holds already
 };
+static_assert(sizeof(PageItem) == 32 && kItemPages * kPageTokens <= 65535, "a plan is read across the bus");
 
 // What the caller asked for that cannot be done (see the messages in pages.cpp).
 enum class BookError { none, id, repeated, length, too_long, busy_dst, src_is_dst, pages, position };
@@ -39,24 +41,34 @@ struct PageBook {
   int32_t max_len = 0, stride = 0;
   std::vector<int32_t> table;  // [ndocs][stride] page ids
   std::vector<int32_t> len;    // [ndocs] tokens
-  std::vector<int32_t> ref;    // [npages] documents that hold the page
-  std::vector<int32_t> spare;  // free pages, the next one last; never grows past npages
+  std::vector<int32_t> more;   // [npages] documents that hold the page, beyond the first
+  std::vector<int32_t> spare;  // free pages: the first `top` entries, the next one last
+  int64_t top = 0, shared = 0;  // shared: sum of `more`
   std::vector<uint32_t> stamp;
   uint32_t epoch = 0;
 
   static int64_t pages_of(int64_t tokens) { return (tokens + kPageTokens - 1) / kPageTokens; }
+  // Page ids are copied eight at a time, so that documents of a few pages take no
+  // branch for each: rows of the table are whole eights, and what a copy reads or
+  // writes beyond its n entries is nobody's.
+  static int32_t row_pages(int32_t max_len) { return (int32_t)((pages_of(max_len) + 7) / 8 * 8); }
+  static constexpr int kSlack = 8;
+  static void copy8(int32_t *to, const int32_t *from, int64_t n) {
+    for (int64_t i = 0; i < n; i += 8) std::memcpy(to + i, from + i, 32);
+  }
 
   void init(int64_t npages_, int64_t ndocs_, int32_t max_len_) {
     npages = npages_;
     ndocs = ndocs_;
     max_len = max_len_;
-    stride = (int32_t)pages_of(max_len);
+    stride = row_pages(max_len);
     table.assign((size_t)ndocs * stride, 0);
     len.assign((size_t)ndocs, 0);
-    ref.assign((size_t)npages, 0);
+    more.assign((size_t)npages, 0);
     stamp.assign((size_t)ndocs, 0);
-    spare.resize((size_t)npages);
-    for (int64_t i = 0; i < npages; ++i) spare[i] = (int32_t)(npages - 1 - i);  // lowest page first
+    spare.assign((size_t)npages + kSlack, 0);
+    for (int64_t i = 0; i < npages; ++i) spare[i] = (int32_t)(npages - 1 - i);  // lowest pages first
+    top = npages;
   }
 
   int32_t *row(int64_t doc) { return table.data() + (size_t)doc * stride; }
@@ -78,22 +90,35 @@ struct PageBook {
   }
   bool marked(int64_t id) const { return stamp[id] == epoch; }
 
-  int32_t take() {
-    const int32_t p = spare.back();
-    spare.pop_back();
-    ref[p] = 1;
-    return p;
+  int64_t free_pages() const { return top; }
+  // The next n free pages (there are as many).
+  const int32_t *take(int64_t n) {
+    top -= n;
+    return spare.data() + top;
   }
   void release(int64_t doc) {
     const int32_t *r = row(doc);
-    for (int64_t i = 0, n = pages_of(len[doc]); i < n; ++i)
-      if (--ref[r[i]] == 0) spare.push_back(r[i]);
+    const int64_t n = pages_of(len[doc]);
+    if (shared == 0) {
+      copy8(spare.data() + top, r, n);
+      top += n;
+    } else {
+      for (int64_t i = 0; i < n; ++i) {
+        if (more[r[i]] == 0) {
+          spare[top++] = r[i];
+        } else {
+          --more[r[i]];
+          --shared;
+        }
+      }
+    }
     ntok -= len[doc];
     len[doc] = 0;
   }
 
   // Every plan comes in two steps: a check that changes nothing and counts the
-  // plan's items and page ids, and a commit that cannot fail and writes them.
+  // plan's items and page ids, and a commit that cannot fail and writes them (the
+  // list of page ids has kSlack entries more).
 
   // ---- append: lens[i] tokens to the end of document ids[i]
   BookError check_append(const int64_t *ids, const int32_t *lens, int64_t n, int64_t *at, int64_t *items,
@@ -112,7 +137,7 @@ struct PageBook {
       *pages += span;
       *items += (span + kItemPages - 1) / kItemPages;
     }
-    return fresh > (int64_t)spare.size() ? BookError::pages : BookError::none;
+    return fresh > free_pages() ? BookError::pages : BookError::none;
   }
   // row: first row of document i, i * doc_stride or, packed (0), behind document i - 1's.
   void commit_append(const int64_t *ids, const int32_t *lens, int64_t n, int64_t doc_stride, PageItem *item,
@@ -126,20 +151,30 @@ struct PageBook {
       const int64_t d = ids[i];
       int32_t *t = row(d);
       const int32_t old = len[d], now = old + lens[i];
-      for (int64_t p = pages_of(old); p < pages_of(now); ++p) t[p] = take();
-      for (int32_t p = old / kPageTokens, left = lens[i], fill = old % kPageTokens; left > 0; fill = 0) {
+      const int32_t p0 = old / kPageTokens;  // the first page written, there already if it is partly filled
+      const int64_t fresh = pages_of(now) - pages_of(old);
+      const int32_t *f = take(fresh);
+      if (old == 0) {
+        copy8(t, f, fresh);
+        copy8(page + np, f, fresh);
+      } else {
+        for (int64_t p = 0; p < fresh; ++p) t[pages_of(old) + p] = f[p];
+        for (int64_t p = p0; p < pages_of(now); ++p) page[np + p - p0] = t[p];
+      }
+      for (int32_t p = p0, left = lens[i], fill = old % kPageTokens; left > 0; fill = 0) {
+        const int32_t span = (int32_t)pages_of(fill + left);
         PageItem w;
         w.doc = (int32_t)d;
         w.first = p;
-        w.npages = (int32_t)pages_of(fill + left) < kItemPages ? (int32_t)pages_of(fill + left) : kItemPages;
+        w.npages = (uint8_t)(span < kItemPages ? span : kItemPages);
         w.pages = np;
-        w.fill = fill;
-        w.ntok = left < w.npages * kPageTokens - fill ? left : w.npages * kPageTokens - fill;
+        w.fill = (uint8_t)fill;
+        w.ntok = (uint16_t)(left < w.npages * kPageTokens - fill ? left : w.npages * kPageTokens - fill);
         w.row = r;
         left -= w.ntok;
         r += w.ntok;
         if (left == 0) w.len = now;
-        for (int k = 0; k < w.npages; ++k) page[np++] = t[p + k];
+        np += w.npages;
         p += w.npages;
         *item++ = w;
       }
@@ -161,7 +196,7 @@ struct PageBook {
       if (l < 0 || l > len[src[i]]) return BookError::length;
       fresh += l % kPageTokens != 0;
     }
-    return fresh > (int64_t)spare.size() ? BookError::pages : BookError::none;
+    return fresh > free_pages() ? BookError::pages : BookError::none;
   }
   // An item a document: first = whole pages shared, ntok = tokens of the page
   // copied behind them, whose page is `pages` (itself, not a place in a list).
@@ -174,13 +209,14 @@ struct PageBook {
       w.doc = (int32_t)dst[i];
       w.src = (int32_t)src[i];
       w.first = l / kPageTokens;
-      w.ntok = l % kPageTokens;
+      w.ntok = (uint16_t)(l % kPageTokens);
       w.len = l;
       for (int32_t p = 0; p < w.first; ++p) {
         t[p] = s[p];
-        ++ref[s[p]];
+        ++more[s[p]];
       }
-      if (w.ntok) w.pages = t[w.first] = take();
+      shared += w.first;
+      if (w.ntok) w.pages = t[w.first] = *take(1);
       len[dst[i]] = l;
       ntok += l;
       item[i] = w;
@@ -196,7 +232,7 @@ struct PageBook {
     const bool same = &to == this;
     *items = *pages = 0;
     *in_place = false;
-    const int32_t *q = pos;
+    int64_t npos = 0, turns = 0;  // positions; places where one document's follow another's without ascending
     for (int64_t i = 0; i < n; ++i) {
       *at = i;
       if (src[i] < 0 || src[i] >= ndocs) return BookError::id;
@@ -206,43 +242,57 @@ struct PageBook {
       const int32_t have = len[src[i]], l = lens ? lens[i] : have;
       if (l < 0 || l > have) return BookError::length;
       if (l > to.max_len) return BookError::too_long;
-      if (pos) {
-        int32_t before = -1;
-        for (int32_t k = 0; k < l; ++k, ++q) {
-          if (*q <= before || *q >= have) return BookError::position;
-          before = *q;
-        }
+      if (pos && l) {
+        if (pos[npos] < 0 || pos[npos + l - 1] >= have) return BookError::position;
+        turns += npos && pos[npos] <= pos[npos - 1];
+        npos += l;
       }
       *in_place |= self;
       *pages += pages_of(l);
       *items += l ? (pages_of(l) + kItemPages - 1) / kItemPages : self;
     }
-    return *pages > (int64_t)to.spare.size() ? BookError::pages : BookError::none;
+    if (pos) {  // ascending everywhere else: one pass over all positions
+      for (int64_t k = 1; k < npos;) {
+        int32_t falls = 0;
+        const int64_t stop = npos - k < (1 << 20) ? npos : k + (1 << 20);
+        for (; k < stop; ++k) falls += pos[k] <= pos[k - 1];
+        turns -= falls;
+      }
+      if (turns) {
+        int64_t k = 0;
+        for (int64_t i = 0; i < n; ++i)
+          for (const int64_t first = k, stop = k + lens[i]; k < stop; ++k)
+            if (k > first && pos[k] <= pos[k - 1]) {
+              *at = i;
+              return BookError::position;
+            }
+      }
+    }
+    return *pages > to.free_pages() ? BookError::pages : BookError::none;
   }
   void commit_copy(const int64_t *src, PageBook &to, const int64_t *dst, const int32_t *lens, const int32_t *pos,
                    int64_t n, PageItem *item, int32_t *page) {
     // old pages of documents copied onto themselves are read by this plan: they
     // go back only after every new page is taken
+    int64_t all = 0;
+    for (int64_t i = 0; i < n; ++i) all += pages_of(lens ? lens[i] : len[src[i]]);
+    std::memcpy(page, to.take(all), (size_t)all * 4);
     int32_t np = 0;
-    for (int64_t i = 0; i < n; ++i)
-      for (int64_t p = pages_of(lens ? lens[i] : len[src[i]]); p > 0; --p) page[np++] = to.take();
     int64_t at = 0;
-    np = 0;
     for (int64_t i = 0; i < n; ++i) {
       const bool self = &to == this && src[i] == dst[i];
       const int32_t l = lens ? lens[i] : len[src[i]];
       const int32_t base = np;
       np += (int32_t)pages_of(l);
       if (self) release(src[i]);
-      int32_t *t = to.row(dst[i]);
-      for (int32_t p = 0; p < np - base; ++p) t[p] = page[base + p];
+      copy8(to.row(dst[i]), page + base, np - base);
       for (int32_t done = 0; done < l || (l == 0 && self);) {
         PageItem w;
         w.doc = (int32_t)dst[i];
         w.src = (int32_t)src[i];
         w.first = done / kPageTokens;
-        w.ntok = l - done < kItemPages * kPageTokens ? l - done : kItemPages * kPageTokens;
-        w.npages = (int32_t)pages_of(w.ntok);
+        w.ntok = (uint16_t)(l - done < kItemPages * kPageTokens ? l - done : kItemPages * kPageTokens);
+        w.npages = (uint8_t)pages_of(w.ntok);
         w.pages = base + w.first;
         w.row = pos ? at + done : done;
         done += w.ntok;
@@ -274,8 +324,8 @@ struct PageBook {
         PageItem w;
         w.doc = (int32_t)ids[i];
         w.first = done / kPageTokens;
-        w.ntok = l - done < kItemPages * kPageTokens ? l - done : kItemPages * kPageTokens;
-        w.npages = (int32_t)pages_of(w.ntok);
+        w.ntok = (uint16_t)(l - done < kItemPages * kPageTokens ? l - done : kItemPages * kPageTokens);
+        w.npages = (uint8_t)pages_of(w.ntok);
         w.row = r;
         done += w.ntok;
         r += w.ntok;

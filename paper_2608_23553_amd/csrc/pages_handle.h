@@ -10,9 +10,10 @@ constexpr int64_t kPagesMaxItems = (1 << 24) - 1;  // work items of a launch (25
 
 // Pinned host memory that calls' plans lie in, taken from the front to the back
 // of two halves in turn.  Behind the last call of a half an event is recorded;
-// the half is used again once that has passed.
+// the half is used again once that has passed.  Small plans are read by the
+// kernels from there, larger ones from a copy at the same place of `dev`.
 struct PlanRing {
-  char *host = nullptr;
+  char *host = nullptr, *dev = nullptr;
   size_t half = 0;  // bytes of each half
   size_t used = 0;  // of the current half
   int cur = 0;

@@ -52,14 +52,15 @@ struct Store {
       }
     }
     CHECK(ntok == book.ntok);
-    int64_t spare = 0;
+    int64_t spare = 0, more = 0;
     for (int64_t p = 0; p < book.npages; ++p) {
-      CHECK(ref[p] == book.ref[p]);
+      CHECK((ref[p] ? ref[p] - 1 : 0) == book.more[p]);
       spare += ref[p] == 0;
+      more += book.more[p];
     }
-    std::vector<int32_t> f = book.spare;
+    std::vector<int32_t> f(book.spare.begin(), book.spare.begin() + book.top);
     std::sort(f.begin(), f.end());
-    CHECK((int64_t)f.size() == spare && std::unique(f.begin(), f.end()) == f.end());
+    CHECK(more == book.shared && (int64_t)f.size() == spare && std::unique(f.begin(), f.end()) == f.end());
     for (int32_t p : f) CHECK(ref[p] == 0);
   }
 
@@ -68,9 +69,8 @@ struct Store {
     if (BookError e = book.check_append(ids.data(), lens.data(), ids.size(), &at, &ni, &np); e != BookError::none)
       return e;
     std::vector<PageItem> it(ni + 1);
-    Lens page(np + 1);
+    Lens page(np + PageBook::kSlack);
     it[ni].doc = -99;
-    page[np] = -99;
     std::vector<int> rows;  // the tensor
     for (size_t i = 0; i < ids.size(); ++i) {
       if (stride) rows.resize(i * stride, -2);
@@ -81,7 +81,7 @@ struct Store {
     }
     (void)packed;
     book.commit_append(ids.data(), lens.data(), ids.size(), stride, it.data(), page.data());
-    CHECK(it[ni].doc == -99 && page[np] == -99);
+    CHECK(it[ni].doc == -99);
     for (int64_t j = 0; j < ni; ++j) {
       const PageItem &w = it[j];
       CHECK(w.npages >= 1 && w.npages <= kItemPages && w.ntok >= 1 && w.pages + w.npages <= np);
@@ -140,11 +140,10 @@ struct Store {
     }
     for (size_t i = 0; i < src.size(); ++i) to.plain[dst[i]] = made[i];
     std::vector<PageItem> it(ni + 1);
-    Lens page(np + 1);
+    Lens page(np + PageBook::kSlack);
     it[ni].doc = -99;
-    page[np] = -99;
     book.commit_copy(src.data(), to.book, dst.data(), l, q, src.size(), it.data(), page.data());
-    CHECK(it[ni].doc == -99 && page[np] == -99);
+    CHECK(it[ni].doc == -99);
     // every write before any read would show a page that is both; so do the items backwards too
     const std::vector<int> old = pool;
     for (int64_t j = ni - 1; j >= 0; --j) {
@@ -256,17 +255,17 @@ static void refusals() {
   CHECK(s.fork({0, 0}, {1, 1}, nullptr) == BookError::repeated && s.fork({4}, {1}, nullptr) == BookError::id);
   CHECK(s.fork({0, 1}, {1, 2}, nullptr) == BookError::src_is_dst);
   CHECK(s.fork({0, 0}, {1, 2}, nullptr) == BookError::none);  // two pages shared by three, a third each
-  CHECK(s.book.spare.size() == 1);
+  CHECK(s.book.free_pages() == 1);
   CHECK(s.copy({1}, s, {3}, nullptr, nullptr) == BookError::pages);
   CHECK(s.copy({1}, s, {3}, &l2, &back) == BookError::position && s.copy({1}, s, {3}, &l2, &down) == BookError::position);
   CHECK(s.copy({1}, s, {3}, &l2, &far) == BookError::position && s.copy({0}, s, {1}, &l20, nullptr) == BookError::busy_dst);
   CHECK(s.copy({0, 0}, s, {0, 3}, &l51, nullptr) == BookError::src_is_dst);
   s.check();
-  CHECK(s.copy({0}, s, {0}, &l2, nullptr) == BookError::none && s.book.spare.size() == 1);
+  CHECK(s.copy({0}, s, {0}, &l2, nullptr) == BookError::none && s.book.free_pages() == 1);
   s.check();
   s.drop({0, 1, 1, 2});
   s.check();
-  CHECK(s.book.spare.size() == 6 && s.book.ntok == 0);
+  CHECK(s.book.free_pages() == 6 && s.book.ntok == 0);
 }
 
 int main() {
