@@ -13,7 +13,14 @@ struct DeviceGuard {
   int prev = -1;
   bool ok = false;
   explicit DeviceGuard(int dev) {
-    if (hipGetDevice(&prev) == hipSuccess && hipSetDevice(dev) == hipSuccess) ok = true;
+    if (hipGetDevice(&prev) != hipSuccess) {
+      prev = -1;
+    } else if (prev == dev) {
+      prev = -1;  // nothing to restore
+      ok = true;
+    } else {
+      ok = hipSetDevice(dev) == hipSuccess;
+    }
   }
   ~DeviceGuard() {
     if (prev >= 0) (void)hipSetDevice(prev);
