@@ -39,7 +39,7 @@ enum class BookError { none, id, repeated, length, too_long, busy_dst, src_is_ds
 struct PageBook {
   int64_t npages = 0, ndocs = 0, ntok = 0;
   int32_t max_len = 0, stride = 0;
-  std::vector<int32_t> table;  // [ndocs][stride] page ids
+  std::vector<int32_t> table;  // [ndocs][stride] page ids, kSlack more
   std::vector<int32_t> len;    // [ndocs] tokens
   std::vector<int32_t> more;   // [npages] documents that hold the page, beyond the first
   std::vector<int32_t> spare;  // free pages: the first `top` entries, the next one last
@@ -62,7 +62,7 @@ struct PageBook {
     ndocs = ndocs_;
     max_len = max_len_;
     stride = row_pages(max_len);
-    table.assign((size_t)ndocs * stride, 0);
+    table.assign((size_t)ndocs * stride + kSlack, 0);
     len.assign((size_t)ndocs, 0);
     more.assign((size_t)npages, 0);
     stamp.assign((size_t)ndocs, 0);
@@ -103,13 +103,13 @@ struct PageBook {
       copy8(spare.data() + top, r, n);
       top += n;
     } else {
-      for (int64_t i = 0; i < n; ++i) {
-        if (more[r[i]] == 0) {
-          spare[top++] = r[i];
-        } else {
-          --more[r[i]];
-          --shared;
-        }
+      for (int64_t i = 0; i < n; ++i) {  // without a branch: shared or not is a coin's toss
+        int32_t &m = more[r[i]];
+        const bool last = m == 0;
+        spare[top] = r[i];
+        top += last;
+        m -= !last;
+        shared -= !last;
       }
     }
     ntok -= len[doc];
@@ -154,13 +154,9 @@ struct PageBook {
       const int32_t p0 = old / kPageTokens;  // the first page written, there already if it is partly filled
       const int64_t fresh = pages_of(now) - pages_of(old);
       const int32_t *f = take(fresh);
-      if (old == 0) {
-        copy8(t, f, fresh);
-        copy8(page + np, f, fresh);
-      } else {
-        for (int64_t p = 0; p < fresh; ++p) t[pages_of(old) + p] = f[p];
-        for (int64_t p = p0; p < pages_of(now); ++p) page[np + p - p0] = t[p];
-      }
+      if (pages_of(old) + (fresh + 7) / 8 * 8 <= stride) copy8(t + pages_of(old), f, fresh);
+      else std::memcpy(t + pages_of(old), f, (size_t)fresh * 4);
+      copy8(page + np, t + p0, pages_of(now) - p0);
       for (int32_t p = p0, left = lens[i], fill = old % kPageTokens; left > 0; fill = 0) {
         const int32_t span = (int32_t)pages_of(fill + left);
         PageItem w;
@@ -211,10 +207,8 @@ struct PageBook {
       w.first = l / kPageTokens;
       w.ntok = (uint16_t)(l % kPageTokens);
       w.len = l;
-      for (int32_t p = 0; p < w.first; ++p) {
-        t[p] = s[p];
-        ++more[s[p]];
-      }
+      copy8(t, s, w.first);
+      for (int32_t p = 0; p < w.first; ++p) ++more[s[p]];
       shared += w.first;
       if (w.ntok) w.pages = t[w.first] = *take(1);
       len[dst[i]] = l;
