@@ -457,7 +457,8 @@ typedef struct {
   int32_t device;       /* HIP device ordinal */
 } chimera_pages_info;
 
-/* npages, ndocs 1 .. 2^31 - 1, max_len 1 .. CHIMERA_PAGES_MAX_LEN.  Host memory:
+/* npages 1 .. 252,645,135 (275 GB), ndocs 1 .. 2^31 - 1, max_len 1 ..
+ * CHIMERA_PAGES_MAX_LEN.  Host memory:
  * 8 npages + 8 ndocs (1 + 4 ceil(max_len / 128)) bytes. */
 int chimera_pages_create(int hip_device, int64_t npages, int64_t ndocs, int32_t max_len, chimera_pages **out);
 void chimera_pages_free(chimera_pages *pg); /* NULL-safe; waits for pending work */

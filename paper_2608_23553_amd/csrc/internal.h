@@ -236,6 +236,7 @@ int fixed_scratch(int device, void **ptr);
 // plans of pages_book.h; they may lie in host memory that the device can read.
 // X rows of 128 values, ld values apart; out of the read [rows][128].
 constexpr int kPageBytes = 16 * 68;
+constexpr int64_t kPagesMaxPages = 252645135;  // page * kPageBytes / 64 in 32 bits: 275 GB of pages
 struct PagesView {
   uint8_t *pool = nullptr;   // [npages][kPageBytes]
   int32_t *table = nullptr;  // [ndocs][stride] page ids

@@ -340,14 +340,24 @@ struct PageOperand {
   uint4 code[2];
   int scale;
 };
-// Pages a (rows 0 .. 15, lanes with bit 4 clear) and b (rows 16 .. 31).
-__device__ __forceinline__ PageOperand load_pages(const uint8_t *__restrict__ pool, int32_t a, int32_t b) {
-  const int lane = lane_id(), t = lane & 15, h = lane >> 5;
-  const uint8_t *p = pool + (int64_t)(lane & 16 ? b : a) * kPageBytes;
+// Pages a (rows 0 .. 15, lanes with bit 4 clear) and b (rows 16 .. 31), as units of
+// 64 bytes from the pool's start; codes, scales: this lane's place in page 0.
+struct PageBase {
+  const uint8_t *codes, *scales;
+  __device__ explicit PageBase(const uint8_t *pool) {
+    const int t = lane_id() & 15, h = lane_id() >> 5;
+    codes = pool + code_at(h, t);
+    scales = pool + scale_at(h, t);
+  }
+};
+constexpr uint32_t kPageUnits = kPageBytes / 64;
+static_assert(kPageUnits * 64 == kPageBytes && kPagesMaxPages == 0xFFFFFFFFu / kPageUnits, "units in 32 bits");
+__device__ __forceinline__ PageOperand load_pages(const PageBase &base, uint32_t a, uint32_t b) {
+  const uint64_t at = (uint64_t)(lane_id() & 16 ? b : a) << 6;
   PageOperand o;
-  o.code[0] = *(const uint4 *)(p + code_at(h, t));
-  o.code[1] = *(const uint4 *)(p + code_at(h + 2, t));
-  o.scale = *(const uint16_t *)(p + scale_at(h, t));
+  o.code[0] = *(const uint4 *)(base.codes + at);
+  o.code[1] = *(const uint4 *)(base.codes + at + (code_at(2, 0) - code_at(0, 0)));
+  o.scale = *(const uint16_t *)(base.scales + at);
   return o;
 }
 
@@ -472,8 +482,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
   const int rank = __builtin_popcountll(some & ((1ull << lane) - 1));
   const int entry = __builtin_amdgcn_ds_permute((np ? rank : 63 - (lane - rank)) * 4, lane);
 
-  // lane j: the id of page w0 + j of the string, and whether a document ends there
-  auto window = [&](uint32_t w0, uint64_t &ends) -> int32_t {
+  // lane j: where page w0 + j of the string is, in units, and whether a document ends there
+  auto window = [&](uint32_t w0, uint64_t &ends) -> uint32_t {
     const uint32_t at = w0 + lane;
     int e = 0;  // entries that end at or before it
 #pragma unroll
@@ -485,11 +495,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
     const int64_t r = ((int64_t)__shfl((int)(row >> 32), e, 64) << 32) | (uint32_t)__shfl((int)(uint32_t)row, e, 64);
     const uint32_t stop = (uint32_t)__shfl((int)end, e, 64);  // by every lane: lane e may have no page here
     ends = __ballot(at < total && at + 1 == stop);
-    return at < total ? table[r + at] : 0;
+    return at < total ? (uint32_t)table[r + at] * kPageUnits : 0;
   };
 
   uint64_t ends, next_ends = 0;
-  int32_t page = window(0, ends), next_page = 0;  // under way while the query is prepared
+  uint32_t page = window(0, ends), next_page = 0;  // under way while the query is prepared
 
   const int64_t step = (int64_t)q_stride * CHIMERA_DIM;
   const bool wide = __syncthreads_or(
@@ -510,6 +520,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
   }
   if (some == 0) return;
 
+  const PageBase base(pool);
   float m[NB];
 #pragma unroll
   for (int u = 0; u < NB; ++u) m[u] = -INFINITY;
@@ -555,8 +566,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
     if (w0 + 64 < total) next_page = window(w0 + 64, next_ends);
     // behind the last page its own id stands again
     auto fetch = [&](int t) {
-      return load_pages(pool, __builtin_amdgcn_readlane(page, min(2 * t, cnt - 1)),
-                        __builtin_amdgcn_readlane(page, min(2 * t + 1, cnt - 1)));
+      return load_pages(base, (uint32_t)__builtin_amdgcn_readlane((int)page, min(2 * t, cnt - 1)),
+                        (uint32_t)__builtin_amdgcn_readlane((int)page, min(2 * t + 1, cnt - 1)));
     };
     PageOperand a[DEPTH];
 #pragma unroll

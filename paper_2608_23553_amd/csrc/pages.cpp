@@ -137,8 +137,9 @@ int chimera_pages_create(int hip_device, int64_t npages, int64_t ndocs, int32_t 
   if (!out) return fail(CHIMERA_E_INVAL, "null argument");
   if (npages < 1 || ndocs < 1 || max_len < 1)
     return fail(CHIMERA_E_INVAL, "npages, ndocs and max_len must be >= 1");
-  if (npages > INT32_MAX || ndocs > INT32_MAX || max_len > CHIMERA_PAGES_MAX_LEN)
-    return fail(CHIMERA_E_UNSUPPORTED, "npages or ndocs above 2^31 - 1, or max_len above %d", CHIMERA_PAGES_MAX_LEN);
+  if (npages > kPagesMaxPages || ndocs > INT32_MAX || max_len > CHIMERA_PAGES_MAX_LEN)
+    return fail(CHIMERA_E_UNSUPPORTED, "npages above %lld, ndocs above 2^31 - 1 or max_len above %d",
+                (long long)kPagesMaxPages, CHIMERA_PAGES_MAX_LEN);
   int ndev = 0;
   if (hipGetDeviceCount(&ndev) != hipSuccess || ndev <= 0) {
     (void)hipGetLastError();

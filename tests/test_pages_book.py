@@ -39,7 +39,7 @@ def test_null_arguments_are_rejected_without_gpu():
 
 @pytest.mark.parametrize("npages,ndocs,max_len,code", [
     (0, 1, 1, chimera.E_INVAL), (1, 0, 1, chimera.E_INVAL), (1, 1, 0, chimera.E_INVAL), (-1, 1, 1, chimera.E_INVAL),
-    (2**31, 1, 1, chimera.E_UNSUPPORTED), (1, 2**31, 1, chimera.E_UNSUPPORTED),
+    (252_645_136, 1, 1, chimera.E_UNSUPPORTED), (1, 2**31, 1, chimera.E_UNSUPPORTED),
     (1, 1, 2**20 + 1, chimera.E_UNSUPPORTED)])
 def test_sizes_that_a_store_cannot_have(npages, ndocs, max_len, code):
     with pytest.raises(ChimeraError) as e:
