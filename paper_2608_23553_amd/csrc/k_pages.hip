@@ -249,77 +249,96 @@ struct QueryOperand {
 // they are in registers), digit 2 [step][lane][6], exponents [step][lane].
 constexpr int LOW_WORDS = 2 * 2 * 64 * 6, HIGH_WORDS = 2 * 64 * 6 + 2 * 64;
 
-// All 256 threads: the operands of NB blocks of 32 tokens into LDS, low [NB]
-// [LOW_WORDS] and high [NB][HIGH_WORDS]: of one query or, PAIR, of one query each
-// (`next` values apart); tokens at or past Tq are zero.  Returns whether this
-// thread's block has a third digit.
+// A thread makes half a block: 16 values of one token.  Its values as they lie in
+// memory, for each of NB blocks of 32 tokens: of one query or, PAIR, of one query
+// each (`next` values apart); zero for tokens at or past Tq.
+template <int NB, bool F32>
+struct QueryRaw {
+  uint4 v[NB][F32 ? 4 : 2];
+};
+__device__ __forceinline__ int half_step() { return (int)threadIdx.x >> 7; }
+__device__ __forceinline__ int half_lane() { return ((int)threadIdx.x >> 1) & 63; }
 template <int NB, bool PAIR, bool F32>
-__device__ __forceinline__ bool prepare_query(const char *__restrict__ Q0, int64_t next, int Tq, uint32_t *low,
-                                              uint32_t *high) {
-  static_assert(NB <= 2, "a thread a lane of a block's step");
-  bool wide = false;
-  if (const int u = (int)threadIdx.x; u < NB * 128) {
-    const int blk = u >> 7, step = (u >> 6) & 1, l = u & 63, d0 = 64 * step + 32 * (l >> 5);
-    const int j = (PAIR ? 0 : blk * 32) + (l & 31);
-    const char *Q = Q0 + (PAIR && blk ? next : 0) * (F32 ? 4 : 2);
-    float k[32];
+__device__ __forceinline__ void fetch_query(const char *__restrict__ Q, int64_t next, int Tq, QueryRaw<NB, F32> &raw) {
+  const int d0 = 64 * half_step() + 32 * (half_lane() >> 5) + 16 * ((int)threadIdx.x & 1);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) k[i] = 0.0f;
-    if (j < Tq) {
-      if constexpr (F32) {
-        const float4 *src = (const float4 *)((const float *)Q + (int64_t)j * CHIMERA_DIM + d0);
+  for (int blk = 0; blk < NB; ++blk) {
+    const int j = (PAIR ? 0 : blk * 32) + (half_lane() & 31);
+    const int64_t at = (PAIR && blk ? next : 0) + (int64_t)j * CHIMERA_DIM + d0;
+    const uint4 *src = (const uint4 *)(Q + at * (F32 ? 4 : 2));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float4 v = src[i];
-          const float y[4] = {v.x, v.y, v.z, v.w};
+    for (int i = 0; i < (F32 ? 4 : 2); ++i) raw.v[blk][i] = j < Tq ? src[i] : make_uint4(0, 0, 0, 0);
+  }
+}
+
+// All 256 threads: the operands of the blocks into LDS, low [NB][LOW_WORDS] and
+// high [NB][HIGH_WORDS].  Returns whether one of this thread's has a third digit.
+template <int NB, bool F32>
+__device__ __forceinline__ bool prepare_query(const QueryRaw<NB, F32> &raw, uint32_t *low0, uint32_t *high0) {
+  const int half = (int)threadIdx.x & 1, l = half_lane(), step = half_step();
+  bool any = false;
 #pragma unroll
-          for (int m = 0; m < 4; ++m) k[4 * i + m] = __uint_as_float((uint32_t)grid_bf16_bits(y[m]) << 16) * 2048.0f;
-        }
-      } else {
-        const uint4 *src = (const uint4 *)((const uint16_t *)Q + (int64_t)j * CHIMERA_DIM + d0);
+  for (int blk = 0; blk < NB; ++blk) {
+    float k[16];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint4 v = src[i];
-          const uint32_t y[4] = {v.x, v.y, v.z, v.w};
+    for (int i = 0; i < (F32 ? 4 : 2); ++i) {
+      const uint4 v = raw.v[blk][i];
+      const uint32_t y[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-          for (int m = 0; m < 4; ++m) {
-            // below 1/16 rounded onto the grid; above it every bf16 is on it
-            k[8 * i + 2 * m] = rintf(__uint_as_float(y[m] << 16) * 2048.0f);
-            k[8 * i + 2 * m + 1] = rintf(__uint_as_float(y[m] & 0xFFFF0000u) * 2048.0f);
-          }
+      for (int m = 0; m < 4; ++m) {
+        if constexpr (F32) {
+          k[4 * i + m] = __uint_as_float((uint32_t)grid_bf16_bits(__uint_as_float(y[m])) << 16) * 2048.0f;
+        } else {
+          // below 1/16 rounded onto the grid; above it every bf16 is on it
+          k[8 * i + 2 * m] = rintf(__uint_as_float(y[m] << 16) * 2048.0f);
+          k[8 * i + 2 * m + 1] = rintf(__uint_as_float(y[m] & 0xFFFF0000u) * 2048.0f);
         }
       }
     }
     float top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) top = fmaxf(top, fabsf(k[i]));
-    const int shift = min(max((int)(__float_as_uint(top) >> 23) - 127 - 13, 0), 100);
-    const float down = __uint_as_float((uint32_t)(127 - shift) << 23);
-    wide = top > 1024.0f;
-    f32x16 dig[3][2];  // even and odd dimensions, as the conversion takes them
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(k[i]));
+    top = fmaxf(top, shfl_xor(top, 1));  // of the block's other half
+    f32x16 dig[3][2] = {};  // even and odd dimensions, as the conversion takes them, and as many zeros
+    int shift = 0;
+    if (top <= 512.0f) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const float x = rintf(k[i] * down);
-      const float a2 = wide ? rintf(x * (1.0f / 1024.0f)) : 0.0f, r = x - 1024.0f * a2;
-      const float a1 = fabsf(r) > 512.0f ? 2.0f * rintf(r * (1.0f / 64.0f)) : rintf(r * (1.0f / 32.0f));
-      dig[2][i & 1][i >> 1] = a2;
-      dig[1][i & 1][i >> 1] = a1;
-      dig[0][i & 1][i >> 1] = r - 32.0f * a1;
+      for (int i = 0; i < 16; ++i) {
+        const float a1 = rintf(k[i] * (1.0f / 32.0f));
+        dig[1][i & 1][i >> 1] = a1;
+        dig[0][i & 1][i >> 1] = k[i] - 32.0f * a1;
+      }
+    } else {
+      const bool wide = top > 1024.0f;
+      any |= wide;
+      shift = min(max((int)(__float_as_uint(top) >> 23) - 127 - 13, 0), 100);
+      const float down = __uint_as_float((uint32_t)(127 - shift) << 23);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float x = rintf(k[i] * down);
+        const float a2 = wide ? rintf(x * (1.0f / 1024.0f)) : 0.0f, r = x - 1024.0f * a2;
+        const float a1 = fabsf(r) > 512.0f ? 2.0f * rintf(r * (1.0f / 64.0f)) : rintf(r * (1.0f / 32.0f));
+        dig[2][i & 1][i >> 1] = a2;
+        dig[1][i & 1][i >> 1] = a1;
+        dig[0][i & 1][i >> 1] = r - 32.0f * a1;
+      }
     }
-    low += blk * LOW_WORDS;
-    high += blk * HIGH_WORDS;
+    uint32_t *low = low0 + blk * LOW_WORDS, *high = high0 + blk * HIGH_WORDS;
 #pragma unroll
     for (int m = 0; m < 3; ++m) {
       const v6u32 c = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(dig[m][0], dig[m][1], 8.0f);
-      uint32_t *o = m < 2 ? low + ((step * 2 + m) * 64 + l) * 6 : high + (step * 64 + l) * 6;
+      // The conversion reads its sources while it writes: they are kept alive behind
+      // it, so that the compiler does not put the result in their registers.
+      asm volatile("" ::"v"(dig[m][0]), "v"(dig[m][1]), "v"(c));
+      uint32_t *o = (m < 2 ? low + ((step * 2 + m) * 64 + l) * 6 : high + (step * 64 + l) * 6) + 3 * half;
 #pragma unroll
-      for (int i = 0; i < 6; ++i) o[i] = c[i];
+      for (int i = 0; i < 3; ++i) o[i] = c[i];  // the first 16 of 32
     }
     // digit m counts 8 * 32^m / 2048 * 2^shift
     const uint32_t e = (uint32_t)(127 + 3 - 11 + shift);
-    high[2 * 64 * 6 + step * 64 + l] = e | (e + 5) << 8 | (e + 10) << 16;
+    if (half == 0) high[2 * 64 * 6 + step * 64 + l] = e | (e + 5) << 8 | (e + 10) << 16;
   }
-  return wide;
+  return any;
 }
 
 __device__ __forceinline__ void load_query(const uint32_t *low, const uint32_t *high, QueryOperand &q) {
@@ -427,11 +446,12 @@ __global__ __launch_bounds__(256) void k_pages_unscored(int32_t *__restrict__ id
 // belong to, and DEPTH tiles are under way.  A document's maxima over its rows
 // stay in registers until its last page, then go to a ring in LDS; 16 documents
 // at a time are summed over the query tokens, four lanes each, in the same order
-// whatever NB is.
+// whatever NB is.  SPLIT: the four waves take a quarter each of the pages of the
+// same (up to 16) entries, and their maxima meet in LDS.
 constexpr int DEPTH = 4, FLUSH = 16, RING = 32;
 static_assert(FLUSH + 2 * DEPTH <= RING, "documents that end within DEPTH tiles have room");
 
-template <int NB, bool PAIR, bool F32, bool KEYS>
+template <int NB, bool PAIR, bool SPLIT, bool F32, bool KEYS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4 : 3))) void k_pages_score(const void *__restrict__ Q, int Tq, int q_stride,
                                                      const int32_t *__restrict__ ids, int64_t ld,
                                                      const int32_t *__restrict__ n_valid, int64_t n, int64_t nq,
@@ -460,9 +480,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
   }
   const int64_t q = group * PER;
   const int64_t last = n_valid ? min(n, (int64_t)n_valid[q]) : n;
-  if (chunk * 4 * per_wave >= last) return;  // the whole workgroup
+  if (chunk * (SPLIT ? 1 : 4) * per_wave >= last) return;  // the whole workgroup
   const bool two = PAIR && q + 1 < nq;
-  const int64_t c0 = (chunk * 4 + wave) * per_wave;
+  const int64_t step = (int64_t)q_stride * CHIMERA_DIM;
+  QueryRaw<NB, F32> raw;  // under way while the list and the page table are read
+  fetch_query<NB, PAIR, F32>((const char *)Q + q * step * (F32 ? 4 : 2), two ? step : 0, Tq, raw);
+  const int64_t c0 = (SPLIT ? chunk : chunk * 4 + wave) * per_wave;
   // lane e: entry c0 + e, its document's row of the page table and its pages
   const bool on = lane < per_wave && c0 + lane < last;
   int64_t row = 0;
@@ -473,6 +496,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
       row = doc * stride;
       np = (uint32_t)(lens[doc] + 15) >> 4;
     }
+  }
+  const bool none = np == 0;
+  const uint64_t full = __ballot(!none);  // entries that have pages
+  if constexpr (SPLIT) {
+    const uint32_t quarter = (np + 3) >> 2, first = min(wave * quarter, np);
+    row += first;
+    np = min(np - first, quarter);
   }
   const uint64_t some = __ballot(np > 0);
   const uint32_t end = wave_incl_scan(np);
@@ -501,9 +531,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
   uint64_t ends, next_ends = 0;
   uint32_t page = window(0, ends), next_page = 0;  // under way while the query is prepared
 
-  const int64_t step = (int64_t)q_stride * CHIMERA_DIM;
-  const bool wide = __syncthreads_or(
-      prepare_query<NB, PAIR, F32>((const char *)Q + q * step * (F32 ? 4 : 2), two ? step : 0, Tq, low, high));
+  const bool wide = __syncthreads_or(prepare_query<NB, F32>(raw, low, high));
   QueryOperand op[NB];
 #pragma unroll
   for (int u = 0; u < NB; ++u) load_query(low + u * LOW_WORDS, high + u * HIGH_WORDS, op[u]);
@@ -514,11 +542,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
     if constexpr (KEYS) ((int32_t *)out)[(q + u) * n + c] = score_key(F);
     else ((float *)out)[(q + u) * n + c] = F;
   };
-  if (on && np == 0) {
+  if (on && none && !(SPLIT && wave)) {
     put(c0 + lane, 0, -INFINITY);
     if (two) put(c0 + lane, 1, -INFINITY);
   }
-  if (some == 0) return;
+  if (full == 0) return;  // SPLIT: the whole workgroup
+  if constexpr (SPLIT) {
+    for (int i = lane; i < FLUSH * ROW; i += 64) best_of[i] = -INFINITY;
+    __builtin_amdgcn_wave_barrier();
+  }
 
   const PageBase base(pool);
   float m[NB];
@@ -528,7 +560,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
   auto sum_up = [&]() {
     __builtin_amdgcn_wave_barrier();
     constexpr int LANES = 64 / FLUSH, EACH = NB * 32 / LANES;  // lanes of a document, query tokens of a lane
-    const int i = summed + lane / LANES, part = lane % LANES;
+    const int i = summed + lane / LANES, part = lane % LANES;  // SPLIT: entry i, else the i-th that has pages
     float sum = 0.0f;
 #pragma unroll
     for (int k = 0; k < EACH; k += 8) {
@@ -536,15 +568,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int tok = part * EACH + k + j;
-        const float x = best_of[(i % RING) * ROW + tok];
+        float x = best_of[(i % RING) * ROW + tok];
+        if constexpr (SPLIT)
+#pragma unroll
+          for (int w = 1; w < 4; ++w) x = fmaxf(x, best_of[(w * RING + i) * ROW + tok]);
         s8 += (PAIR ? tok & 31 : tok) < Tq ? x : 0.0f;
       }
       sum = k ? sum + s8 : s8;
     }
     sum += shfl_xor(sum, 1);
     if constexpr (!PAIR) sum += shfl_xor(sum, 2);
-    const int64_t c = c0 + __shfl(entry, i & 63, 64);
-    if (i < ended) {
+    const int64_t c = c0 + (SPLIT ? i : __shfl(entry, i & 63, 64));
+    if (SPLIT ? (full >> i) & 1 : i < ended) {
       if (part == 0) put(c, 0, sum);
       if (PAIR && part == 2 && two) put(c, 1, sum);
     }
@@ -552,10 +587,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
     summed = min(summed + FLUSH, ended);
   };
   auto page_done = [&]() {  // the document's last page: its maxima go to LDS
+    const int slot = SPLIT ? __builtin_amdgcn_readlane(entry, ended) : ended % RING;
 #pragma unroll
     for (int u = 0; u < NB; ++u) {
       const float x = fmaxf(m[u], shfl_xor(m[u], 32));
-      if (lane < 32) best_of[(ended % RING) * ROW + u * 32 + lane] = x;
+      if (lane < 32) best_of[slot * ROW + u * 32 + lane] = x;
       m[u] = -INFINITY;
     }
     ++ended;
@@ -599,12 +635,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
         // behind the branch, so that the registers of a tile stay where they are
         a[d] = fetch(t + DEPTH);
       }
-      if (ended - summed >= FLUSH) sum_up();
+      if (!SPLIT && ended - summed >= FLUSH) sum_up();
     }
     page = next_page;
     ends = next_ends;
   }
-  while (summed < ended) sum_up();
+  if constexpr (SPLIT) {
+    __syncthreads();
+    if (wave == 0) sum_up();
+  } else {
+    while (summed < ended) sum_up();
+  }
 }
 
 // ------------------------------------------------------------ launchers
@@ -669,33 +710,33 @@ static int score_entries(int64_t n, int64_t groups, bool shared) {
   return (int)std::max<int64_t>(1, std::min<int64_t>(shared ? 64 : 16, n * groups / 4096));
 }
 
-template <int NB, bool PAIR>
+template <int NB, bool PAIR, bool SPLIT>
 static void launch_score_t(const void *Q, int q_dtype, int64_t nq, int Tq, int q_stride, const int32_t *ids,
                            int64_t ld, const int32_t *n_valid, int64_t n, const PagesView &pg, void *out, bool keys,
                            hipStream_t s) {
   const int64_t groups = PAIR ? (nq + 1) / 2 : nq;
-  const int per_wave = score_entries(n, groups, !ids || ld == 0);
-  int64_t chunks = (n + 4 * per_wave - 1) / (4 * per_wave);
+  const int per_wave = SPLIT ? 1 : score_entries(n, groups, !ids || ld == 0), per_group = SPLIT ? 1 : 4 * per_wave;
+  int64_t chunks = (n + per_group - 1) / per_group;
   if (chunks >= 8) chunks = (chunks + 7) / 8 * 8;
   const dim3 grid((unsigned)(chunks * groups));
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, Q, Tq, q_stride, ids, ld, n_valid, n, nq, per_wave, chunks, pg.pool,
-                       pg.table, pg.stride, pg.lens, pg.ndocs, out);
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, Q, Tq, q_stride, ids, ld, n_valid, n, nq, per_wave, chunks,
+                       pg.pool, pg.table, pg.stride, pg.lens, pg.ndocs, out);
   };
-  if constexpr (PAIR) {
-    if (q_dtype == CHIMERA_F32) go(k_pages_score<NB, PAIR, true, false>);
-    else go(k_pages_score<NB, PAIR, false, false>);
-  } else {
-    if (keys) go(k_pages_score<NB, PAIR, false, true>);
-    else if (q_dtype == CHIMERA_F32) go(k_pages_score<NB, PAIR, true, false>);
-    else go(k_pages_score<NB, PAIR, false, false>);
-  }
+  if constexpr (!PAIR)
+    if (keys) return go(k_pages_score<NB, PAIR, SPLIT, false, true>);
+  if (q_dtype == CHIMERA_F32) go(k_pages_score<NB, PAIR, SPLIT, true, false>);
+  else go(k_pages_score<NB, PAIR, SPLIT, false, false>);
 }
 
 void launch_pages_score(const void *Q, int q_dtype, int64_t nq, int Tq, int q_stride, const int32_t *ids, int64_t ld,
                         const int32_t *n_valid, int64_t n, const PagesView &pg, void *out, bool keys, hipStream_t s) {
   if (nq <= 0 || n <= 0) return;
-  const bool pair = Tq <= 32 && nq > 1 && (!ids || ld == 0) && !keys;
+  // no more entries than CUs: a workgroup each (1 x 256 documents of 64, 512 and 2000
+  // tokens: 6.8, 7.2 and 10.2 us, 6.8, 9.2 and 19.6 with a wave each; 1 x 1000
+  // documents: 9.6, 11.1 and 25.9 against 7.0, 10.5 and 26.5)
+  const bool split = n * nq <= 256;
+  const bool pair = !split && Tq <= 32 && nq > 1 && (!ids || ld == 0) && !keys;
   // a launch counts its work-items in 32 bits: queries in batches of an even number
   const int64_t few = std::max<int64_t>(1, n / 64 + 8);  // workgroups of a query where there are more than 4096 waves
   const int64_t per = std::max<int64_t>(2, (((int64_t)1 << 23) / few) & ~(int64_t)1);
@@ -706,9 +747,11 @@ void launch_pages_score(const void *Q, int q_dtype, int64_t nq, int Tq, int q_st
     const int32_t *nv = n_valid ? n_valid + q0 : nullptr;
     char *o = (char *)out + (size_t)q0 * n * 4;
     auto go = [&](auto launch) { launch(Qb, q_dtype, nb, Tq, q_stride, idb, ld, nv, n, pg, o, keys, s); };
-    if (pair) go(launch_score_t<2, true>);
-    else if (Tq <= 32) go(launch_score_t<1, false>);
-    else go(launch_score_t<2, false>);
+    if (split && Tq <= 32) go(launch_score_t<1, false, true>);
+    else if (split) go(launch_score_t<2, false, true>);
+    else if (pair) go(launch_score_t<2, true, false>);
+    else if (Tq <= 32) go(launch_score_t<1, false, false>);
+    else go(launch_score_t<2, false, false>);
   }
 }
 
