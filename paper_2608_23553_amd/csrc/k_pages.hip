@@ -448,7 +448,7 @@ __global__ __launch_bounds__(256) void k_pages_unscored(int32_t *__restrict__ id
 // at a time are summed over the query tokens, four lanes each, in the same order
 // whatever NB is.  SPLIT: the four waves take a quarter each of the pages of the
 // same (up to 16) entries, and their maxima meet in LDS.
-constexpr int DEPTH = 4, FLUSH = 16, RING = 32;
+constexpr int DEPTH = 2, FLUSH = 16, RING = 32;
 static_assert(FLUSH + 2 * DEPTH <= RING, "documents that end within DEPTH tiles have room");
 
 template <int NB, bool PAIR, bool SPLIT, bool F32, bool KEYS>
