@@ -306,16 +306,15 @@ int chimera_pages_copy(chimera_pages *src, const int64_t *src_ids, chimera_pages
   DeviceGuard dg(dst->device);
   if (!dg.ok) return fail(CHIMERA_E_DEVICE, "cannot select device %d", dst->device);
   return guarded([&]() -> int {
-    int64_t at = 0, items = 0, pages = 0, npos = 0;
+    int64_t at = 0, items = 0, pages = 0, npos = 0, turns = 0;
     bool in_place = false;
     if (BookError e = src->book.check_copy(src_ids, dst->book, dst_ids, lens, positions, n, &at, &items, &pages,
-                                           &in_place);
+                                           &npos, &turns, &in_place);
         e != BookError::none)
       return book_fail(e, "copy", dst_ids, at);
     if (items == 0) return CHIMERA_OK;
     if (items > kPagesMaxItems) return fail(CHIMERA_E_UNSUPPORTED, "copy: too many tokens in one call");
     if (int rc = check_stream(s, "copy")) return rc;
-    for (int64_t i = 0; positions && i < n; ++i) npos += lens[i];
     char *plan = nullptr;
     if (int rc = pages_order_before(dst, s)) return rc;
     if (src != dst)
@@ -324,10 +323,9 @@ int chimera_pages_copy(chimera_pages *src, const int64_t *src_ids, chimera_pages
     const size_t ids_at = (size_t)items * sizeof(PageItem), pos_at = ids_at + (size_t)(pages + PageBook::kSlack) * 4;
     const size_t bytes = pos_at + (size_t)npos * (short_pos ? 2 : 4);
     if (int rc = ring_take(dst, bytes, s, &plan)) return rc;
-    if (short_pos)
-      for (int64_t i = 0; i < npos; ++i) ((uint16_t *)(plan + pos_at))[i] = (uint16_t)positions[i];
-    else if (npos)
-      std::memcpy(plan + pos_at, positions, (size_t)npos * 4);
+    if (!(short_pos ? PageBook::take_positions(positions, npos, turns, (uint16_t *)(plan + pos_at))
+                    : PageBook::take_positions(positions, npos, turns, (int32_t *)(plan + pos_at))))
+      return book_fail(BookError::position, "copy", dst_ids, PageBook::falling(lens, positions, n));
     src->book.commit_copy(src_ids, dst->book, dst_ids, lens, positions, n, (PageItem *)plan,
                           (int32_t *)(plan + ids_at));
     const char *p = plan_for_device(dst, plan, bytes, s);

@@ -219,14 +219,16 @@ struct PageBook {
 
   // ---- copy: document dst[i] of `to` becomes tokens pos (ascending; null: the
   // first lens[i]) of document src[i] of this store, in pages of its own.  dst[i]
-  // is empty, or src[i] itself (compaction in place).
+  // is empty, or src[i] itself (compaction in place).  npos: positions in all;
+  // turns: places where one document's follow another's without ascending
+  // (take_positions completes the check).
   BookError check_copy(const int64_t *src, PageBook &to, const int64_t *dst, const int32_t *lens, const int32_t *pos,
-                       int64_t n, int64_t *at, int64_t *items, int64_t *pages, bool *in_place) {
+                       int64_t n, int64_t *at, int64_t *items, int64_t *pages, int64_t *npos, int64_t *turns,
+                       bool *in_place) {
     if (BookError e = to.mark(dst, n, at); e != BookError::none) return e;
     const bool same = &to == this;
-    *items = *pages = 0;
+    *items = *pages = *npos = *turns = 0;
     *in_place = false;
-    int64_t npos = 0, turns = 0;  // positions; places where one document's follow another's without ascending
     for (int64_t i = 0; i < n; ++i) {
       *at = i;
       if (src[i] < 0 || src[i] >= ndocs) return BookError::id;
@@ -237,32 +239,37 @@ struct PageBook {
       if (l < 0 || l > have) return BookError::length;
       if (l > to.max_len) return BookError::too_long;
       if (pos && l) {
-        if (pos[npos] < 0 || pos[npos + l - 1] >= have) return BookError::position;
-        turns += npos && pos[npos] <= pos[npos - 1];
-        npos += l;
+        const int32_t *q = pos + *npos;
+        if (q[0] < 0 || q[l - 1] >= have) return BookError::position;
+        *turns += *npos && q[0] <= q[-1];
+        *npos += l;
       }
       *in_place |= self;
       *pages += pages_of(l);
       *items += l ? (pages_of(l) + kItemPages - 1) / kItemPages : self;
     }
-    if (pos) {  // ascending everywhere else: one pass over all positions
-      for (int64_t k = 1; k < npos;) {
-        int32_t falls = 0;
-        const int64_t stop = npos - k < (1 << 20) ? npos : k + (1 << 20);
-        for (; k < stop; ++k) falls += pos[k] <= pos[k - 1];
-        turns -= falls;
-      }
-      if (turns) {
-        int64_t k = 0;
-        for (int64_t i = 0; i < n; ++i)
-          for (const int64_t first = k, stop = k + lens[i]; k < stop; ++k)
-            if (k > first && pos[k] <= pos[k - 1]) {
-              *at = i;
-              return BookError::position;
-            }
-      }
-    }
     return *pages > to.free_pages() ? BookError::pages : BookError::none;
+  }
+  // The positions as the plan holds them, and whether they ascend but at `turns`
+  // places: one pass without a branch for each document.
+  template <class T>
+  static bool take_positions(const int32_t *pos, int64_t npos, int64_t turns, T *out) {
+    for (int64_t k = 0; k < npos;) {
+      const int64_t stop = npos - k < 4096 ? npos : k + 4096;
+      int32_t falls = 0;
+      for (int64_t j = k ? k : 1; j < stop; ++j) falls += pos[j] <= pos[j - 1];
+      turns -= falls;
+      for (; k < stop; ++k) out[k] = (T)pos[k];
+    }
+    return turns == 0;
+  }
+  // The first document whose positions do not ascend.
+  static int64_t falling(const int32_t *lens, const int32_t *pos, int64_t n) {
+    int64_t k = 0;
+    for (int64_t i = 0; i < n; ++i)
+      for (const int64_t first = k, stop = k + lens[i]; k < stop; ++k)
+        if (k > first && pos[k] <= pos[k - 1]) return i;
+    return 0;
   }
   void commit_copy(const int64_t *src, PageBook &to, const int64_t *dst, const int32_t *lens, const int32_t *pos,
                    int64_t n, PageItem *item, int32_t *page) {

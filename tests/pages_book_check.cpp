@@ -23,6 +23,8 @@ typedef std::vector<int32_t> Lens;
 
 constexpr int FREE = -1;
 
+static int64_t bad_entry = 0;  // of the next call whose positions do not ascend
+
 struct Store {
   PageBook book;
   std::vector<int> pool;                // [npages][16] token numbers, FREE where the scale is NaN
@@ -125,12 +127,21 @@ struct Store {
   }
 
   BookError copy(const Ids &src, Store &to, const Ids &dst, const Lens *lens, const Lens *pos) {
-    int64_t at, ni, np;
+    int64_t at, ni, np, npos, turns;
     bool in_place;
     const int32_t *l = lens ? lens->data() : nullptr, *q = pos ? pos->data() : nullptr;
-    if (BookError e = book.check_copy(src.data(), to.book, dst.data(), l, q, src.size(), &at, &ni, &np, &in_place);
+    if (BookError e = book.check_copy(src.data(), to.book, dst.data(), l, q, src.size(), &at, &ni, &np, &npos, &turns,
+                                      &in_place);
         e != BookError::none)
       return e;
+    if (q) {
+      std::vector<uint16_t> taken(npos);
+      if (!PageBook::take_positions(q, npos, turns, taken.data())) {
+        CHECK(PageBook::falling(l, q, src.size()) == bad_entry);
+        return BookError::position;
+      }
+      CHECK(std::equal(taken.begin(), taken.end(), q));
+    }
     std::vector<std::vector<int>> made;
     for (size_t i = 0, k = 0; i < src.size(); ++i) {
       const std::vector<int> &s = plain[src[i]];
@@ -258,6 +269,15 @@ static void refusals() {
   CHECK(s.book.free_pages() == 1);
   CHECK(s.copy({1}, s, {3}, nullptr, nullptr) == BookError::pages);
   CHECK(s.copy({1}, s, {3}, &l2, &back) == BookError::position && s.copy({1}, s, {3}, &l2, &down) == BookError::position);
+  const Lens l23{2, 3}, second{7, 9, 0, 4, 4}, turn{7, 9, 0, 4, 5};
+  bad_entry = 1;
+  CHECK(s.copy({1, 2}, s, {3, 0}, &l23, &second) != BookError::none);
+  s.drop({0});
+  CHECK(s.copy({1, 2}, s, {3, 0}, &l23, &second) == BookError::position);
+  CHECK(s.copy({1, 2}, s, {3, 0}, &l23, &turn) == BookError::none);
+  s.check();
+  s.drop({0, 3});
+  CHECK(s.fork({1}, {0}, nullptr) == BookError::none);
   CHECK(s.copy({1}, s, {3}, &l2, &far) == BookError::position && s.copy({0}, s, {1}, &l20, nullptr) == BookError::busy_dst);
   CHECK(s.copy({0, 0}, s, {0, 3}, &l51, nullptr) == BookError::src_is_dst);
   s.check();
