@@ -432,7 +432,12 @@ int chimera_search_collab_rabitq(chimera_index *idx, const void *Q, int q_dtype,
  *    fail before anything is launched or changed: E_INVAL for ids out of
  *    range, for an id that is written twice in a call (drop and read allow
  *    repeats) and for lengths out of range, E_NOMEM if the store has too few
- *    free pages.  The arrays may be reused as soon as the call returns.
+ *    free pages, E_UNSUPPORTED above 2^24 - 1 documents or pieces of 256 tokens
+ *    in one call.  The arrays may be reused as soon as the call returns.  What
+ *    the kernels need of them goes through pinned host memory and device memory
+ *    that the store keeps: 1 MiB each or, after a larger call, up to eight times
+ *    that call's plan (32 bytes a document or piece of 256 tokens, 4 a page, 2 or
+ *    4 a position).
  *  - Every call but create, free, info_get and lengths is asynchronous on
  *    hip_stream and comes after all earlier calls on the store, whatever
  *    their streams.  Tensors handed in (X, Q, the score's doc_ids) are read and

@@ -115,10 +115,11 @@ static int book_fail(BookError e, const char *call, const int64_t *ids, int64_t 
 }
 
 // What every call that changes or reads documents by a host list starts with.
-static int check_list(const chimera_pages *pg, const void *ids, int64_t n, const char *call) {
+static int check_list(const chimera_pages *pg, const void *ids, int64_t n, const char *call,
+                      int64_t most = kPagesMaxItems) {
   if (!pg) return fail(CHIMERA_E_INVAL, "null pages");
   if (n < 0 || (n > 0 && !ids)) return fail(CHIMERA_E_INVAL, "%s: null ids or n < 0", call);
-  if (n > INT32_MAX) return fail(CHIMERA_E_UNSUPPORTED, "%s: more than 2^31 - 1 documents", call);
+  if (n > most) return fail(CHIMERA_E_UNSUPPORTED, "%s: more than %lld documents in one call", call, (long long)most);
   return CHIMERA_OK;
 }
 static int check_stream(hipStream_t s, const char *call) {
@@ -214,7 +215,7 @@ int chimera_pages_info_get(const chimera_pages *pg, chimera_pages_info *out) {
 
 int chimera_pages_lengths(const chimera_pages *pg, const int64_t *doc_ids, int64_t n, int32_t *lens,
                           int64_t *total) {
-  if (int rc = check_list(pg, doc_ids, n, "lengths")) return rc;
+  if (int rc = check_list(pg, doc_ids, n, "lengths", INT64_MAX)) return rc;
   for (int64_t i = 0; i < n; ++i)
     if (doc_ids[i] < 0 || doc_ids[i] >= pg->book.ndocs) return book_fail(BookError::id, "lengths", doc_ids, i);
   int64_t sum = 0;

@@ -136,7 +136,7 @@ def test_scores_of_every_query_length(Tq, dtype):
     check_scores(pg.score(Q[1:2], ids[1:2, 5:6]), Q[1:2], docs, lists[1:2, 5:6], "one")
 
 
-@pytest.mark.parametrize("n,nq", [(1, 1), (3, 70), (257, 9), (2000, 2), (999, 33)])
+@pytest.mark.parametrize("n,nq", [(1, 1), (3, 70), (257, 9), (2000, 2), (999, 33), (2, 3001), (256, 1), (85, 3)])
 def test_scores_of_many_documents(n, nq):
     rng = np.random.default_rng(n)
     pg, docs = _filled(rng, rng.integers(0, 40, n), "bf16")
@@ -162,6 +162,31 @@ def test_empty_documents_between_others(pattern):
     lists = torch.arange(n, dtype=torch.int32, device="cuda").repeat(41, 1)
     assert torch.equal(got, pg.score(Q, lists))
     assert torch.equal(got.flip(1)[:, 7:], pg.score(Q, lists.flip(1)[:, 7:]))
+
+
+def test_queries_as_views():
+    """Queries that are strided, transposed or not 16-byte aligned, and repeated documents in a read."""
+    rng = np.random.default_rng(18)
+    pg, docs = _filled(rng, [20, 0, 70])
+    q = tensor(units(rng, 3 * 5 * 2), "bf16").view(3, 10, 128)
+    flat = torch.zeros(3 * 10 * 128 + 3, dtype=torch.bfloat16, device="cuda")
+    flat[3:] = q.flatten()
+    for name, Q in (("every other token", q[:, ::2]), ("some queries", q[::2]), ("token-major", q.transpose(0, 1)),
+                    ("unaligned", flat[3:].view(3, 10, 128)), ("one", q[1:2, 9:])):
+        check_scores(pg.score(Q), Q, docs, [range(3)] * len(Q), name)
+    same(pg.read([2, 0, 1, 2]), np.concatenate([docs[2], docs[0], docs[2]]))
+
+
+@pytest.mark.parametrize("Tq", [20, 50])
+def test_few_long_documents(Tq):
+    """Few entries: four waves share each document, whose pages do not divide evenly."""
+    rng = np.random.default_rng(Tq)
+    lens = [1, 15, 16, 17, 33, 48, 49, 64, 65, 0, 1023, 1024, 1041, 5000]
+    pg, docs = _filled(rng, lens, "bf16")
+    Q = tensor(units(rng, 2 * Tq)).view(2, Tq, 128)
+    check_scores(pg.score(Q), Q, docs, [range(len(lens))] * 2, "few")
+    many = torch.arange(len(lens), dtype=torch.int32, device="cuda").repeat(40)
+    assert torch.equal(pg.score(Q, many)[:, -len(lens):], pg.score(Q))
 
 
 def test_values_that_are_not_finite_never_win():

@@ -65,6 +65,7 @@ def test_search_from_pages(name, ndocs, nq, k):
     ncand = min(w.ncand, w.ndocs // 3)
     ids = _check(idx, pg, docs, q, w.nprobe, ncand, k, name)
     _check(idx, pg, docs, q[:2, :min(7, w.Tq)], w.nprobe, ncand, k, name + " f32, short queries", "f32")
+    _check(idx, pg, docs, q[:1], w.nprobe, min(ncand, 100), 20, name + ", few candidates")
     assert np.mean(ids[:, 0] == src) >= 0.9  # the document that a query was drawn from comes first
 
 
