@@ -370,7 +370,7 @@ class Index:
         Q, dt = self._q(Q)
         nq, Tq, d = Q.shape
         ids, scores = self._results(Q, nq, k, out)
-        _check(lib().chimera_search_pages(self._h, pages._h, _aligned(Q).data_ptr(), dt, nq, Tq, d, nprobe, ncand, k,
+        _check(lib().chimera_search_pages(self._h, pages._h, Q.data_ptr(), dt, nq, Tq, d, nprobe, ncand, k,
                                           ids.data_ptr(), scores.data_ptr(), _stream_ptr(stream)))
         return ids, scores
 
@@ -688,7 +688,8 @@ class Pages:
         if out is None:
             with _on(stream):
                 out = torch.empty((nq, n), dtype=torch.float32, device=self.device)
-        elif tuple(out.shape) != (nq, n) or out.dtype != torch.float32 or out.device != self.device or not out.is_contiguous():
+        elif (tuple(out.shape) != (nq, n) or out.dtype != torch.float32 or out.device != self.device
+              or not out.is_contiguous()):
             raise ValueError(f"out must be a contiguous float32 tensor [{nq}, {n}] on {self.device}")
         _check(self._lib.chimera_pages_score(self._h, Q.data_ptr(), dt, nq, Tq, d, at, n, ld, out.data_ptr(),
                                              self._stream(stream)))

@@ -58,8 +58,9 @@ void launch_pages_plan(const void *host, void *dev, size_t bytes, hipStream_t s)
 // ------------------------------------------------------------ quantising
 // A workgroup takes one item of the plan (up to 16 pages of one document), a
 // wave a page at a time, a lane one block of one token: 32 values, their
-// largest in registers, 16 bytes of codes, one byte of scale.  Bound by memory
-// (256 or 512 bytes read and 68 written a token).
+// largest in registers, 16 bytes of codes, one byte of scale.  Bound by memory, 256
+// or 512 bytes read and 68 written a token: 8,000 documents of 70 bf16 tokens in 42
+// us (4.3 TB/s), 501 of 320 float32 tokens in 20.7 us (4.4 TB/s).
 template <bool F32>
 __global__ __launch_bounds__(256) void k_pages_append(const PageItem *__restrict__ items,
                                                       const int32_t *__restrict__ ids, const void *__restrict__ X,
@@ -123,8 +124,8 @@ __global__ __launch_bounds__(256) void k_pages_append(const PageItem *__restrict
 // ------------------------------------------------------------ reading back
 // A lane takes 8 values of a token, so that a wave writes whole rows: 4 rows
 // of bf16 at a time.  Every value (2 significant bits, exponents from -128) is
-// exact in bf16 and in float32.  Bound by memory (68 bytes read, 256 or 512
-// written a token).
+// exact in bf16 and in float32.  Bound by memory, 68 bytes read and 256 or 512
+// written a token: 8,000 documents of 70 tokens as bf16 in 34 us (5.4 TB/s).
 template <bool F32>
 __global__ __launch_bounds__(256) void k_pages_read(const PageItem *__restrict__ items,
                                                     const uint8_t *__restrict__ pool,
@@ -141,8 +142,9 @@ __global__ __launch_bounds__(256) void k_pages_read(const PageItem *__restrict__
       const uint32_t c = *(const uint32_t *)(page + code_at(b, t) + 4 * (seg & 3));
       const uint32_t s = page[scale_at(b, t)];
       const float sc = scale_float(s);
-      f32x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 1),
-                    __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 3)};
+      const f32x2 v[4] = {
+          __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 1),
+          __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 3)};
       uint32_t y[8];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -163,7 +165,8 @@ __global__ __launch_bounds__(256) void k_pages_read(const PageItem *__restrict__
 
 // ------------------------------------------------------------ sharing and copying
 // A wave a document: its page ids, then the partly filled page behind the
-// shared ones, with free slots behind its ntok tokens.
+// shared ones, with free slots behind its ntok tokens (4,099 documents: 5.3 us,
+// bound by the dependent reads of item, page id and page).
 __global__ __launch_bounds__(64) void k_pages_fork(const PageItem *__restrict__ items, uint8_t *__restrict__ pool,
                                                    int32_t *__restrict__ table, int stride,
                                                    int32_t *__restrict__ lens) {
@@ -183,6 +186,8 @@ __global__ __launch_bounds__(64) void k_pages_fork(const PageItem *__restrict__ 
 }
 
 // Tokens by position into pages of their own; a lane one block of one token.
+// Bound by memory, 68 bytes read and written a token (314,000 tokens of 8,192
+// documents: 13 us, 3.3 TB/s), and for one document by the few workgroups.
 // publish: also the page ids and the length, where no item reads a document
 // that another one writes (else k_pages_publish does, behind it).
 template <class Pos>
@@ -438,29 +443,39 @@ __global__ __launch_bounds__(256) void k_pages_unscored(int32_t *__restrict__ id
   }
 }
 
-// A wave scores list entries one after the other, up to 64 at a time, for NB
-// blocks of 32 query tokens: one query of up to 32 NB tokens or, PAIR, two
+// MaxSim.  A wave scores list entries one after the other, up to 64 of them, for
+// NB blocks of 32 query tokens: one query of up to 32 NB tokens or, PAIR, two
 // queries of up to 32 tokens that share the list (each page is loaded once for
-// both).  The entries' pages are strung together: lane j of a window holds the
-// id of its j-th page, a tile is two neighbouring pages whatever documents they
-// belong to, and DEPTH tiles are under way.  A document's maxima over its rows
-// stay in registers until its last page, then go to a ring in LDS; 16 documents
-// at a time are summed over the query tokens, four lanes each, in the same order
-// whatever NB is.  SPLIT: the four waves take a quarter each of the pages of the
-// same (up to 16) entries, and their maxima meet in LDS.
+// both).  The queries stay in registers and the documents stream through, since a
+// query's operand (6 KB a block) is larger than an average document's pages.  The
+// entries' pages are strung together: lane j of a window has the place of its
+// j-th page, a tile is two neighbouring pages whatever documents they belong to,
+// and DEPTH tiles are under way (2, 3 and 4 are as fast, 6 is 4 to 12% slower).  A
+// document's maxima over its rows stay in registers until its last page, then go
+// to a ring in LDS; 16 documents at a time are summed over the query tokens, four
+// lanes each, in the same order whatever NB is.  SPLIT: a workgroup takes one
+// entry, its waves a quarter of the pages each, and their maxima meet in LDS.
+//
+// What bounds it: with a list for each query the reads that miss L2 (256 x 2048
+// entries of 50,000 documents of 64 tokens: 246 us, 1.79 GB at 7.2 TB/s); with
+// one list for many the matrix cores at the clock that their power allows (64
+// queries x 30,000 documents: 523 us, 1.9 PFLOP/s of useful work, cores busy 51%
+// of the cycles); for few entries the chain of list, length, page table and page
+// (100 documents: 7 us).
 constexpr int DEPTH = 2, FLUSH = 16, RING = 32;
 static_assert(FLUSH + 2 * DEPTH <= RING, "documents that end within DEPTH tiles have room");
 
+// Entries: ids [nq][ld] (null: documents 0 .. n - 1), below n_valid[q] where that
+// is given; out [nq][n], float scores or (KEYS) int32 keys.  An entry that names
+// no document, and a document without a finite token, score -infinity.
 template <int NB, bool PAIR, bool SPLIT, bool F32, bool KEYS>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4 : 3))) void k_pages_score(const void *__restrict__ Q, int Tq, int q_stride,
-                                                     const int32_t *__restrict__ ids, int64_t ld,
-                                                     const int32_t *__restrict__ n_valid, int64_t n, int64_t nq,
-                                                     int per_wave, int64_t chunks, const uint8_t *__restrict__ pool,
-                                                     const int32_t *__restrict__ table, int stride,
-                                                     const int32_t *__restrict__ lens, int64_t ndocs,
-                                                     void *__restrict__ out) {
-  constexpr int PER = PAIR ? 2 : 1;      // queries of a workgroup
-  constexpr int ROW = NB * 32 + 1;       // of the maxima in LDS
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4 : 3))) void k_pages_score(
+    const void *__restrict__ Q, int Tq, int q_stride, const int32_t *__restrict__ ids, int64_t ld,
+    const int32_t *__restrict__ n_valid, int64_t n, int64_t nq, int per_wave, int64_t chunks,
+    const uint8_t *__restrict__ pool, const int32_t *__restrict__ table, int stride, const int32_t *__restrict__ lens,
+    int64_t ndocs, void *__restrict__ out) {
+  constexpr int PER = PAIR ? 2 : 1;  // queries of a workgroup
+  constexpr int ROW = NB * 32 + 1;   // of the maxima in LDS
   static_assert(4 * RING * ROW >= NB * LOW_WORDS, "the maxima take the first digits' place");
   __shared__ uint32_t high[NB * HIGH_WORDS], low[4 * RING * ROW];
   const int lane = lane_id(), wave = (int)(threadIdx.x >> 6);
@@ -548,7 +563,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
   }
   if (full == 0) return;  // SPLIT: the whole workgroup
   if constexpr (SPLIT) {
-    for (int i = lane; i < FLUSH * ROW; i += 64) best_of[i] = -INFINITY;
+    for (int i = lane; i < ROW; i += 64) best_of[i] = -INFINITY;  // a wave may have no page
     __builtin_amdgcn_wave_barrier();
   }
 
@@ -560,7 +575,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
   auto sum_up = [&]() {
     __builtin_amdgcn_wave_barrier();
     constexpr int LANES = 64 / FLUSH, EACH = NB * 32 / LANES;  // lanes of a document, query tokens of a lane
-    const int i = summed + lane / LANES, part = lane % LANES;  // SPLIT: entry i, else the i-th that has pages
+    const int i = summed + lane / LANES, part = lane % LANES;  // the i-th entry that has pages
     float sum = 0.0f;
 #pragma unroll
     for (int k = 0; k < EACH; k += 8) {
@@ -578,8 +593,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
     }
     sum += shfl_xor(sum, 1);
     if constexpr (!PAIR) sum += shfl_xor(sum, 2);
-    const int64_t c = c0 + (SPLIT ? i : __shfl(entry, i & 63, 64));
-    if (SPLIT ? (full >> i) & 1 : i < ended) {
+    const int64_t c = c0 + (SPLIT ? 0 : __shfl(entry, i & 63, 64));
+    if (i < (SPLIT ? 1 : ended)) {
       if (part == 0) put(c, 0, sum);
       if (PAIR && part == 2 && two) put(c, 1, sum);
     }
@@ -587,7 +602,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
     summed = min(summed + FLUSH, ended);
   };
   auto page_done = [&]() {  // the document's last page: its maxima go to LDS
-    const int slot = SPLIT ? __builtin_amdgcn_readlane(entry, ended) : ended % RING;
+    const int slot = ended % RING;
 #pragma unroll
     for (int u = 0; u < NB; ++u) {
       const float x = fmaxf(m[u], shfl_xor(m[u], 32));
@@ -600,7 +615,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
   for (uint32_t w0 = 0; w0 < total; w0 += 64) {
     const int cnt = (int)min(total - w0, 64u), tiles = (cnt + 1) >> 1;
     if (w0 + 64 < total) next_page = window(w0 + 64, next_ends);
-    // behind the last page its own id stands again
+    // behind the last page that one stands again
     auto fetch = [&](int t) {
       return load_pages(base, (uint32_t)__builtin_amdgcn_readlane((int)page, min(2 * t, cnt - 1)),
                         (uint32_t)__builtin_amdgcn_readlane((int)page, min(2 * t + 1, cnt - 1)));
@@ -620,7 +635,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
           if (2 * t + 1 == cnt && (lane & 16)) a[d].scale = 0xFFFF;
           f32x16 s[NB];
 #pragma unroll
-          for (int u = 0; u < NB; ++u) s[u] = page_products(a[d], op[u], wide ? high + u * HIGH_WORDS + lane * 6 : nullptr);
+          for (int u = 0; u < NB; ++u)
+            s[u] = page_products(a[d], op[u], wide ? high + u * HIGH_WORDS + lane * 6 : nullptr);
 #pragma unroll
           for (int u = 0; u < NB; ++u)
 #pragma unroll
@@ -703,9 +719,9 @@ void launch_pages_unscored(int32_t *ids, float *scores, int64_t n, hipStream_t s
 // List entries of a wave: enough waves to fill the chip first (16 a CU), then as
 // many entries as a wave can take (64) where all queries share the list, 16 where
 // each has its own: short chunks keep more of what the queries of a chunk read in
-// an XCD's L2 (256 x 2048 entries of 50,000 documents: 262, 252, 286 and 320 us
-// with 8, 16, 32 and 64 entries; 64 queries x 30,000 documents: 612, 550, 519 and
-// 516 us).
+// an XCD's L2 (256 x 2048 entries of 50,000 documents: 258, 249 and 297 us with 8,
+// 16 and 24 entries; 64 queries x 30,000 documents: 635, 565, 533 and 527 us with 8,
+// 16, 32 and 64).
 static int score_entries(int64_t n, int64_t groups, bool shared) {
   return (int)std::max<int64_t>(1, std::min<int64_t>(shared ? 64 : 16, n * groups / 4096));
 }

@@ -102,7 +102,8 @@ static int book_fail(BookError e, const char *call, const int64_t *ids, int64_t 
     case BookError::none: return CHIMERA_OK;
     case BookError::id: return fail(CHIMERA_E_INVAL, "%s: entry %lld: document id out of range", call, i);
     case BookError::repeated: return fail(CHIMERA_E_INVAL, "%s: entry %lld: document %lld named twice", call, i, id);
-    case BookError::length: return fail(CHIMERA_E_INVAL, "%s: entry %lld: length below 0 or above the document's", call, i);
+    case BookError::length:
+      return fail(CHIMERA_E_INVAL, "%s: entry %lld: length below 0 or above the document's", call, i);
     case BookError::too_long: return fail(CHIMERA_E_INVAL, "%s: entry %lld: document longer than max_len", call, i);
     case BookError::busy_dst: return fail(CHIMERA_E_INVAL, "%s: entry %lld: document %lld is not empty", call, i, id);
     case BookError::src_is_dst:
@@ -260,8 +261,8 @@ int chimera_pages_append(chimera_pages *pg, const int64_t *doc_ids, const int32_
     if (int rc = ring_take(pg, bytes, s, &plan)) return rc;
     pg->book.commit_append(doc_ids, lens, n, doc_stride, (PageItem *)plan, (int32_t *)((PageItem *)plan + items));
     const PageItem *it = (const PageItem *)plan_for_device(pg, plan, bytes, s);
-    launch_pages_append(it, items, (const int32_t *)(it + items), X, x_dtype, ld, pg->view.pool, pg->view.table, pg->view.stride, pg->view.lens,
-                        s);
+    launch_pages_append(it, items, (const int32_t *)(it + items), X, x_dtype, ld, pg->view.pool, pg->view.table,
+                        pg->view.stride, pg->view.lens, s);
     CHIMERA_HIP(hipGetLastError());
     return pages_order_after(pg, s);
   });

@@ -25,7 +25,7 @@ struct PageItem {
   int32_t first = 0;    // its first page here, as a page of the document
   int32_t pages = 0;    // position of their page ids in the plan's list
   int32_t len = -1;     // the document's length after the call; -1: another item sets it
-  int64_t row = 0;      // append, read: first row of the tensor; copy: first position in the plan's list, or first token
+  int64_t row = 0;      // append, read: first row of the tensor; copy: its place in the list of positions, or first token
   int32_t src = 0;      // copy, fork: the document read
   uint16_t ntok = 0;    // tokens to write (read) from there
   uint8_t npages = 0;

@@ -67,7 +67,7 @@ struct Store {
   }
 
   BookError append(const Ids &ids, const Lens &lens, int64_t stride, int &next) {
-    int64_t at, ni, np, packed = 0;
+    int64_t at, ni, np;
     if (BookError e = book.check_append(ids.data(), lens.data(), ids.size(), &at, &ni, &np); e != BookError::none)
       return e;
     std::vector<PageItem> it(ni + 1);
@@ -81,8 +81,7 @@ struct Store {
         plain[ids[i]].push_back(next++);
       }
     }
-    (void)packed;
-    book.commit_append(ids.data(), lens.data(), ids.size(), stride, it.data(), page.data());
+      book.commit_append(ids.data(), lens.data(), ids.size(), stride, it.data(), page.data());
     CHECK(it[ni].doc == -99);
     for (int64_t j = 0; j < ni; ++j) {
       const PageItem &w = it[j];
@@ -220,7 +219,10 @@ static void random_calls(unsigned seed, int64_t npages, int64_t ndocs, int32_t m
     if (what == 0) {
       Lens l;
       int longest = 0;
-      for (int i = 0; i < n; ++i) l.push_back(rnd(0, 2) ? rnd(0, 40) : rnd(0, max_len)), longest = std::max(longest, l.back());
+      for (int i = 0; i < n; ++i) {
+        l.push_back(rnd(0, 2) ? rnd(0, 40) : rnd(0, max_len));
+        longest = std::max(longest, l.back());
+      }
       e = s.append(ids, l, rnd(0, 1) ? 0 : longest + rnd(0, 9), next);
     } else if (what == 1) {
       const Ids src = any();
@@ -268,7 +270,8 @@ static void refusals() {
   CHECK(s.fork({0, 0}, {1, 2}, nullptr) == BookError::none);  // two pages shared by three, a third each
   CHECK(s.book.free_pages() == 1);
   CHECK(s.copy({1}, s, {3}, nullptr, nullptr) == BookError::pages);
-  CHECK(s.copy({1}, s, {3}, &l2, &back) == BookError::position && s.copy({1}, s, {3}, &l2, &down) == BookError::position);
+  CHECK(s.copy({1}, s, {3}, &l2, &back) == BookError::position);
+  CHECK(s.copy({1}, s, {3}, &l2, &down) == BookError::position);
   const Lens l23{2, 3}, second{7, 9, 0, 4, 4}, turn{7, 9, 0, 4, 5};
   bad_entry = 1;
   CHECK(s.copy({1, 2}, s, {3, 0}, &l23, &second) != BookError::none);
@@ -278,7 +281,8 @@ static void refusals() {
   s.check();
   s.drop({0, 3});
   CHECK(s.fork({1}, {0}, nullptr) == BookError::none);
-  CHECK(s.copy({1}, s, {3}, &l2, &far) == BookError::position && s.copy({0}, s, {1}, &l20, nullptr) == BookError::busy_dst);
+  CHECK(s.copy({1}, s, {3}, &l2, &far) == BookError::position);
+  CHECK(s.copy({0}, s, {1}, &l20, nullptr) == BookError::busy_dst);
   CHECK(s.copy({0, 0}, s, {0, 3}, &l51, nullptr) == BookError::src_is_dst);
   s.check();
   CHECK(s.copy({0}, s, {0}, &l2, nullptr) == BookError::none && s.book.free_pages() == 1);

@@ -47,7 +47,8 @@ def test_every_exponent_border_and_special_value(dtype):
     finite values, infinities and NaN."""
     rng = np.random.default_rng(3)
     borders = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0])
-    near = np.concatenate([borders, np.nextafter(borders.astype(np.float32), 9), np.nextafter(borders.astype(np.float32), 0)])
+    b32 = borders.astype(np.float32)
+    near = np.concatenate([borders, np.nextafter(b32, 9), np.nextafter(b32, 0)])
     rows = []
     for e in range(-149, 128):
         m = rng.uniform(4, 8, (4, 32)) * rng.choice([-1, 1], (4, 32))
