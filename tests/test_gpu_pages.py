@@ -421,6 +421,61 @@ def test_score_in_a_graph():
         torch.cuda.synchronize()
 
 
+def test_more_queries_than_one_launch_takes():
+    """300,000 documents of one token: a launch takes 1,786 queries."""
+    rng = np.random.default_rng(19)
+    n, nq = 300_000, 1790
+    X = tensor(units(rng, 5000), "bf16").repeat(n // 5000, 1)
+    pg = Pages(n, n, 1)
+    pg.append(np.arange(n), X, np.ones(n, np.int32))
+    Q = tensor(units(rng, nq), "bf16").view(nq, 1, 128)
+    got = pg.score(Q)
+    for q in (0, 1, 1785, 1786, 1789):
+        assert torch.equal(got[q], pg.score(Q[q:q + 1])[0]), q
+    ids = torch.arange(n - 1, -1, -1, dtype=torch.int32, device="cuda").expand(nq, n)
+    own = pg.score(Q, ids)
+    assert torch.equal(own, got.flip(1))
+    v = mx_values(host(X[:5000]))
+    check_scores(got[:2, :5000], Q[:2], [t[None] for t in v], [range(5000)] * 2)
+
+
+def test_two_host_threads():
+    """Calls of two threads on one store: each is done or refused as busy, and the store stays whole."""
+    import threading
+    rng = np.random.default_rng(20)
+    x = units(rng, 64)
+    X, v = tensor(x), mx_values(x)
+    pg = Pages(4000, 2000, 64)
+    a, b = np.arange(1000), np.arange(1000, 2000)
+    lens = np.ones(1000, np.int32)
+    one = X[:1].expand(1000, 128).contiguous()
+    errors = []
+
+    def work(ids):
+        done = 0
+        for _ in range(400):
+            try:
+                pg.append(ids, one, lens)
+                done += 1
+            except ChimeraError as e:
+                if e.code != chimera.E_BUSY:
+                    errors.append(e)
+            if done == 5:
+                break
+        counts.append(done)
+
+    counts = []
+    threads = [threading.Thread(target=work, args=(ids,)) for ids in (a, b)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors and all(counts)
+    got = pg.lengths()
+    assert sorted({tuple(set(got[:1000])), tuple(set(got[1000:]))}) == sorted({(c,) for c in counts})
+    same(pg.read([0, 1999]), np.repeat(v[:1], got[0] + got[1999], 0))
+
+
 def test_many_calls_without_waiting():
     """More calls under way than plan buffers, over several stores."""
     rng = np.random.default_rng(16)
@@ -478,7 +533,8 @@ def test_refusals_leave_everything_as_it_was():
                   lambda: pg.append([2], X.half(), [64]), lambda: pg.append([2], X.cpu(), [64]),
                   lambda: pg.append([2], X.view(1, 64, 128), [65]), lambda: pg.fork([0, 1], [2]),
                   lambda: pg.copy([0], [2], None, [1]), lambda: pg.copy([0], [2], [2], [1]),
-                  lambda: pg.score(X), lambda: pg.score(Q.double()), lambda: pg.score(Q, torch.zeros(1, 3, device="cuda")),
+                  lambda: pg.score(X), lambda: pg.score(Q.double()),
+                  lambda: pg.score(Q, torch.zeros(1, 3, device="cuda")),
                   lambda: pg.score(Q, torch.zeros(2, 3, dtype=torch.int32, device="cuda")),
                   lambda: pg.score(Q, out=torch.zeros(1, 4, device="cuda")),
                   lambda: pg.read([0], out=torch.zeros(19, 128, device="cuda"))):
