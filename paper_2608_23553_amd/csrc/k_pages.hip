@@ -255,24 +255,26 @@ struct QueryOperand {
 constexpr int LOW_WORDS = 2 * 2 * 64 * 6, HIGH_WORDS = 2 * 64 * 6 + 2 * 64;
 
 // A thread makes half a block: 16 values of one token.  Its values as they lie in
-// memory, for each of NB blocks of 32 tokens: of one query or, PAIR, of one query
-// each (`next` values apart); zero for tokens at or past Tq.
+// memory, for each of NB blocks of 32 tokens: token g of the blocks is token
+// g % 2^slot of query g >> slot, `next` values a query; zero where that is at or
+// past Tq, or the query past the `have` there are.
 template <int NB, bool F32>
 struct QueryRaw {
   uint4 v[NB][F32 ? 4 : 2];
 };
 __device__ __forceinline__ int half_step() { return (int)threadIdx.x >> 7; }
 __device__ __forceinline__ int half_lane() { return ((int)threadIdx.x >> 1) & 63; }
-template <int NB, bool PAIR, bool F32>
-__device__ __forceinline__ void fetch_query(const char *__restrict__ Q, int64_t next, int Tq, QueryRaw<NB, F32> &raw) {
+template <int NB, bool F32>
+__device__ __forceinline__ void fetch_query(const char *__restrict__ Q, int64_t next, int slot, int have, int Tq,
+                                            QueryRaw<NB, F32> &raw) {
   const int d0 = 64 * half_step() + 32 * (half_lane() >> 5) + 16 * ((int)threadIdx.x & 1);
 #pragma unroll
   for (int blk = 0; blk < NB; ++blk) {
-    const int j = (PAIR ? 0 : blk * 32) + (half_lane() & 31);
-    const int64_t at = (PAIR && blk ? next : 0) + (int64_t)j * CHIMERA_DIM + d0;
-    const uint4 *src = (const uint4 *)(Q + at * (F32 ? 4 : 2));
+    const int g = blk * 32 + (half_lane() & 31), u = g >> slot, j = g & ((1 << slot) - 1);
+    const uint4 *src = (const uint4 *)(Q + (u * next + (int64_t)j * CHIMERA_DIM + d0) * (F32 ? 4 : 2));
+    const bool on = j < Tq && u < have;
 #pragma unroll
-    for (int i = 0; i < (F32 ? 4 : 2); ++i) raw.v[blk][i] = j < Tq ? src[i] : make_uint4(0, 0, 0, 0);
+    for (int i = 0; i < (F32 ? 4 : 2); ++i) raw.v[blk][i] = on ? src[i] : make_uint4(0, 0, 0, 0);
   }
 }
 
@@ -444,17 +446,21 @@ __global__ __launch_bounds__(256) void k_pages_unscored(int32_t *__restrict__ id
 }
 
 // MaxSim.  A wave scores list entries one after the other, up to 64 of them, for
-// NB blocks of 32 query tokens: one query of up to 32 NB tokens or, PAIR, two
-// queries of up to 32 tokens that share the list (each page is loaded once for
-// both).  The queries stay in registers and the documents stream through, since a
-// query's operand (6 KB a block) is larger than an average document's pages.  The
-// entries' pages are strung together: lane j of a window has the place of its
-// j-th page, a tile is two neighbouring pages whatever documents they belong to,
-// and DEPTH tiles are under way (2, 3 and 4 are as fast, 6 is 4 to 12% slower).  A
-// document's maxima over its rows stay in registers until its last page, then go
-// to a ring in LDS; 16 documents at a time are summed over the query tokens, four
-// lanes each, in the same order whatever NB is.  SPLIT: a workgroup takes one
-// entry, its waves a quarter of the pages each, and their maxima meet in LDS.
+// NB blocks of 32 query tokens: one query of up to 32 NB tokens or, PACK, several
+// that share the list, each in 2^slot >= Tq places of the blocks: a page is loaded
+// and multiplied once for all of them (64 queries x 30,000 documents of 64 tokens:
+// 36, 85, 148 and 264 us with 1, 4, 8 and 16 query tokens; 371, 381, 410 and 477
+// with two queries at a time).  PACK 2 is two queries of 32 places, known when it
+// is compiled (1.2% faster there).  The queries stay in registers and the documents
+// stream through, since a query's operand (6 KB a block) is larger than an average
+// document's pages.  The entries' pages are strung together: lane j of a window has
+// the place of its j-th page, a tile is two neighbouring pages whatever documents
+// they belong to, and DEPTH tiles are under way (2, 3 and 4 are as fast, 6 is 4 to
+// 12% slower).  A document's maxima over its rows stay in registers until its last
+// page, then go to a ring in LDS; 16 documents at a time are summed over the query
+// tokens, four lanes each, in the same order whatever NB and PACK are.  SPLIT: a
+// workgroup takes one entry, its waves a quarter of the pages each, and their
+// maxima meet in LDS.
 //
 // What bounds it: with a list for each query the reads that miss L2 (256 x 2048
 // entries of 50,000 documents of 64 tokens: 246 us, 1.79 GB at 7.2 TB/s); with
@@ -468,14 +474,15 @@ static_assert(FLUSH + 2 * DEPTH <= RING, "documents that end within DEPTH tiles 
 // Entries: ids [nq][ld] (null: documents 0 .. n - 1), below n_valid[q] where that
 // is given; out [nq][n], float scores or (KEYS) int32 keys.  An entry that names
 // no document, and a document without a finite token, score -infinity.
-template <int NB, bool PAIR, bool SPLIT, bool F32, bool KEYS>
+template <int NB, int PACK, bool SPLIT, bool F32, bool KEYS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4 : 3))) void k_pages_score(
     const void *__restrict__ Q, int Tq, int q_stride, const int32_t *__restrict__ ids, int64_t ld,
-    const int32_t *__restrict__ n_valid, int64_t n, int64_t nq, int per_wave, int64_t chunks,
+    const int32_t *__restrict__ n_valid, int n, int nq, int any_slot, int per_wave, int chunks,
     const uint8_t *__restrict__ pool, const int32_t *__restrict__ table, int stride, const int32_t *__restrict__ lens,
     int64_t ndocs, void *__restrict__ out) {
-  constexpr int PER = PAIR ? 2 : 1;  // queries of a workgroup
-  constexpr int ROW = NB * 32 + 1;   // of the maxima in LDS
+  constexpr int ROW = NB * 32 + 1;  // of the maxima in LDS
+  const int slot = PACK == 2 ? 5 : any_slot;
+  const int per = PACK ? NB * 32 >> slot : 1;  // queries of a workgroup
   static_assert(4 * RING * ROW >= NB * LOW_WORDS, "the maxima take the first digits' place");
   __shared__ uint32_t high[NB * HIGH_WORDS], low[4 * RING * ROW];
   const int lane = lane_id(), wave = (int)(threadIdx.x >> 6);
@@ -483,30 +490,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
   // entries for each wave) stays with one XCD, all queries' workgroups for it one
   // behind the other: lists that ascend name about the same documents there,
   // some of which its L2 still holds.
-  const int64_t groups = (nq + PER - 1) / PER;
-  int64_t chunk, group;
-  if (chunks % 8 == 0) {
-    const int64_t k = blockIdx.x >> 3;
-    chunk = (k / groups) * 8 + (blockIdx.x & 7);
-    group = k % groups;
-  } else {
-    chunk = blockIdx.x / groups;
-    group = blockIdx.x % groups;
-  }
-  const int64_t q = group * PER;
-  const int64_t last = n_valid ? min(n, (int64_t)n_valid[q]) : n;
+  const int groups = PACK ? (nq + per - 1) / per : nq, wg = (int)blockIdx.x;
+  const bool dealt = chunks % 8 == 0;
+  const int k = dealt ? wg >> 3 : wg;
+  const int chunk = dealt ? k / groups * 8 + (wg & 7) : k / groups;
+  const int64_t q = (int64_t)(k % groups) * per;
+  const int last = !PACK && n_valid ? min(n, n_valid[q]) : n;
   if (chunk * (SPLIT ? 1 : 4) * per_wave >= last) return;  // the whole workgroup
-  const bool two = PAIR && q + 1 < nq;
+  const int have = PACK ? min(per, nq - (int)q) : 1;
   const int64_t step = (int64_t)q_stride * CHIMERA_DIM;
   QueryRaw<NB, F32> raw;  // under way while the list and the page table are read
-  fetch_query<NB, PAIR, F32>((const char *)Q + q * step * (F32 ? 4 : 2), two ? step : 0, Tq, raw);
-  const int64_t c0 = (SPLIT ? chunk : chunk * 4 + wave) * per_wave;
+  fetch_query<NB, F32>((const char *)Q + q * step * (F32 ? 4 : 2), step, PACK ? slot : 6, have, Tq, raw);
+  const int c0 = (SPLIT ? chunk : chunk * 4 + wave) * per_wave;
   // lane e: entry c0 + e, its document's row of the page table and its pages
   const bool on = lane < per_wave && c0 + lane < last;
   int64_t row = 0;
   uint32_t np = 0;
   if (on) {
-    const int64_t doc = ids ? (int64_t)ids[q * ld + c0 + lane] : c0 + lane;
+    const int64_t doc = ids ? ids[(PACK ? 0 : q * ld) + c0 + lane] : c0 + lane;
     if (doc >= 0 && doc < ndocs) {
       row = doc * stride;
       np = (uint32_t)(lens[doc] + 15) >> 4;
@@ -553,14 +554,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
   __syncthreads();
   float *best_of = (float *)low + wave * RING * ROW;
 
-  auto put = [&](int64_t c, int u, float F) {
-    if constexpr (KEYS) ((int32_t *)out)[(q + u) * n + c] = score_key(F);
-    else ((float *)out)[(q + u) * n + c] = F;
+  void *const out_q = (uint32_t *)out + q * n;
+  auto put = [&](int c, int u, float F) {
+    const int64_t at = (PACK ? (int64_t)u * n : 0) + c;
+    if constexpr (KEYS) ((int32_t *)out_q)[at] = score_key(F);
+    else ((float *)out_q)[at] = F;
   };
-  if (on && none && !(SPLIT && wave)) {
-    put(c0 + lane, 0, -INFINITY);
-    if (two) put(c0 + lane, 1, -INFINITY);
-  }
+  if (on && none && !(SPLIT && wave))
+    for (int u = 0; u < have; ++u) put(c0 + lane, u, -INFINITY);
   if (full == 0) return;  // SPLIT: the whole workgroup
   if constexpr (SPLIT) {
     for (int i = lane; i < ROW; i += 64) best_of[i] = -INFINITY;  // a wave may have no page
@@ -576,27 +577,42 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4
     __builtin_amdgcn_wave_barrier();
     constexpr int LANES = 64 / FLUSH, EACH = NB * 32 / LANES;  // lanes of a document, query tokens of a lane
     const int i = summed + lane / LANES, part = lane % LANES;  // the i-th entry that has pages
-    float sum = 0.0f;
+    const bool on = i < (SPLIT ? 1 : ended);
+    const int c = c0 + (SPLIT ? 0 : __shfl(entry, i & 63, 64));
+    const int places = PACK ? 1 << slot : NB * 32, u0 = PACK ? part * EACH >> slot : 0;  // of a query; this lane's first query
+    auto best = [&](int j) {  // the maximum of this lane's j-th token, 0 for one past its query's
+      const int tok = part * EACH + j;
+      float x = best_of[(i % RING) * ROW + tok];
+      if constexpr (SPLIT)
 #pragma unroll
-    for (int k = 0; k < EACH; k += 8) {
-      float s8 = 0.0f;
+        for (int w = 1; w < 4; ++w) x = fmaxf(x, best_of[(w * RING + i) * ROW + tok]);
+      return (tok & (places - 1)) < Tq ? x : 0.0f;
+    };
+    if (PACK && places < 8) {
+#pragma unroll 1
+      for (int j0 = 0; j0 < EACH; j0 += 4) {
+        const float x[4] = {best(j0), best(j0 + 1), best(j0 + 2), best(j0 + 3)};
+        float sum = 0.0f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int tok = part * EACH + k + j;
-        float x = best_of[(i % RING) * ROW + tok];
-        if constexpr (SPLIT)
-#pragma unroll
-          for (int w = 1; w < 4; ++w) x = fmaxf(x, best_of[(w * RING + i) * ROW + tok]);
-        s8 += (PAIR ? tok & 31 : tok) < Tq ? x : 0.0f;
+        for (int j = 0; j < 4; ++j) {
+          sum += x[j];
+          const int u = u0 + ((j0 + j) >> slot);
+          if ((j & (places - 1)) == places - 1) {
+            if (on && u < have) put(c, u, sum);
+            sum = 0.0f;
+          }
+        }
       }
-      sum = k ? sum + s8 : s8;
-    }
-    sum += shfl_xor(sum, 1);
-    if constexpr (!PAIR) sum += shfl_xor(sum, 2);
-    const int64_t c = c0 + (SPLIT ? 0 : __shfl(entry, i & 63, 64));
-    if (i < (SPLIT ? 1 : ended)) {
-      if (part == 0) put(c, 0, sum);
-      if (PAIR && part == 2 && two) put(c, 1, sum);
+    } else {
+      float s8[2] = {0.0f, 0.0f};
+#pragma unroll
+      for (int j = 0; j < EACH; ++j) s8[j / 8] += best(j);
+      float sum = s8[0];
+      if (EACH == 16 && places >= 16) sum += s8[1];
+      if (places >= 2 * EACH) sum += shfl_xor(sum, 1);
+      if (places >= 4 * EACH) sum += shfl_xor(sum, 2);
+      if (on && (part * EACH & (places - 1)) == 0 && u0 < have) put(c, u0, sum);
+      if (EACH == 16 && places == 8 && on && u0 + 1 < have) put(c, u0 + 1, s8[1]);
     }
     __builtin_amdgcn_wave_barrier();
     summed = min(summed + FLUSH, ended);
@@ -726,23 +742,25 @@ static int score_entries(int64_t n, int64_t groups, bool shared) {
   return (int)std::max<int64_t>(1, std::min<int64_t>(shared ? 64 : 16, n * groups / 4096));
 }
 
-template <int NB, bool PAIR, bool SPLIT>
+template <int NB, int PACK, bool SPLIT>
 static void launch_score_t(const void *Q, int q_dtype, int64_t nq, int Tq, int q_stride, const int32_t *ids,
-                           int64_t ld, const int32_t *n_valid, int64_t n, const PagesView &pg, void *out, bool keys,
-                           hipStream_t s) {
-  const int64_t groups = PAIR ? (nq + 1) / 2 : nq;
+                           int64_t ld, const int32_t *n_valid, int64_t n, const PagesView &pg, int slot, void *out,
+                           bool keys, hipStream_t s) {
+  const int per = PACK ? NB * 32 >> slot : 1;
+  const int64_t groups = (nq + per - 1) / per;
   const int per_wave = SPLIT ? 1 : score_entries(n, groups, !ids || ld == 0), per_group = SPLIT ? 1 : 4 * per_wave;
   int64_t chunks = (n + per_group - 1) / per_group;
   if (chunks >= 8) chunks = (chunks + 7) / 8 * 8;
   const dim3 grid((unsigned)(chunks * groups));
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, Q, Tq, q_stride, ids, ld, n_valid, n, nq, per_wave, chunks,
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, Q, Tq, q_stride, ids, ld, n_valid, (int)n, (int)nq, slot, per_wave,
+                       (int)chunks,
                        pg.pool, pg.table, pg.stride, pg.lens, pg.ndocs, out);
   };
-  if constexpr (!PAIR)
-    if (keys) return go(k_pages_score<NB, PAIR, SPLIT, false, true>);
-  if (q_dtype == CHIMERA_F32) go(k_pages_score<NB, PAIR, SPLIT, true, false>);
-  else go(k_pages_score<NB, PAIR, SPLIT, false, false>);
+  if constexpr (!PACK)
+    if (keys) return go(k_pages_score<NB, PACK, SPLIT, false, true>);
+  if (q_dtype == CHIMERA_F32) go(k_pages_score<NB, PACK, SPLIT, true, false>);
+  else go(k_pages_score<NB, PACK, SPLIT, false, false>);
 }
 
 void launch_pages_score(const void *Q, int q_dtype, int64_t nq, int Tq, int q_stride, const int32_t *ids, int64_t ld,
@@ -752,22 +770,30 @@ void launch_pages_score(const void *Q, int q_dtype, int64_t nq, int Tq, int q_st
   // tokens: 6.8, 7.2 and 10.2 us, 6.8, 9.2 and 19.6 with a wave each; 1 x 1000
   // documents: 9.6, 11.1 and 25.9 against 7.0, 10.5 and 26.5)
   const bool split = n * nq <= 256;
-  const bool pair = !split && Tq <= 32 && nq > 1 && (!ids || ld == 0) && !keys;
-  // a launch counts its work-items in 32 bits: queries in batches of an even number
-  const int64_t few = std::max<int64_t>(1, n / 64 + 8);  // workgroups of a query where there are more than 4096 waves
-  const int64_t per = std::max<int64_t>(2, (((int64_t)1 << 23) / few) & ~(int64_t)1);
+  // queries that share the list lie side by side in the blocks, in one block if
+  // that holds them all
+  const bool pack = !split && Tq <= 32 && nq > 1 && (!ids || ld == 0) && !keys;
+  int slot = 0;
+  while (1 << slot < Tq) ++slot;
+  const bool one = nq << slot <= 32;
+  const int group = pack ? (one ? 32 : 64) >> slot : 1;
+  // a launch counts its work-items in 32 bits: whole groups of queries
+  const int64_t few = n / 64 + 8;  // workgroups of a group where there are more than 4096 waves, at most
+  const int64_t per = std::max<int64_t>(1, ((int64_t)1 << 23) / few) * group;
   for (int64_t q0 = 0; q0 < nq; q0 += per) {
     const int64_t nb = std::min(per, nq - q0);
     const char *Qb = (const char *)Q + (size_t)q0 * q_stride * CHIMERA_DIM * (q_dtype == CHIMERA_F32 ? 4 : 2);
     const int32_t *idb = ids ? ids + q0 * ld : nullptr;
     const int32_t *nv = n_valid ? n_valid + q0 : nullptr;
     char *o = (char *)out + (size_t)q0 * n * 4;
-    auto go = [&](auto launch) { launch(Qb, q_dtype, nb, Tq, q_stride, idb, ld, nv, n, pg, o, keys, s); };
-    if (split && Tq <= 32) go(launch_score_t<1, false, true>);
-    else if (split) go(launch_score_t<2, false, true>);
-    else if (pair) go(launch_score_t<2, true, false>);
-    else if (Tq <= 32) go(launch_score_t<1, false, false>);
-    else go(launch_score_t<2, false, false>);
+    auto go = [&](auto launch) { launch(Qb, q_dtype, nb, Tq, q_stride, idb, ld, nv, n, pg, slot, o, keys, s); };
+    if (split && Tq <= 32) go(launch_score_t<1, 0, true>);
+    else if (split) go(launch_score_t<2, 0, true>);
+    else if (pack && one) go(launch_score_t<1, 1, false>);
+    else if (pack && slot == 5) go(launch_score_t<2, 2, false>);
+    else if (pack) go(launch_score_t<2, 1, false>);
+    else if (Tq <= 32) go(launch_score_t<1, 0, false>);
+    else go(launch_score_t<2, 0, false>);
   }
 }
 

@@ -165,6 +165,46 @@ def test_empty_documents_between_others(pattern):
     assert torch.equal(got.flip(1)[:, 7:], pg.score(Q, lists.flip(1)[:, 7:]))
 
 
+@pytest.mark.parametrize("nq", [2, 5, 16, 33, 130])
+@pytest.mark.parametrize("Tq", [1, 2, 3, 4, 5, 8, 9, 16, 17])
+def test_short_queries_that_share_a_list(Tq, nq):
+    """Many queries side by side score as each does alone: also with one that has large values or none that are finite
+    among them, empty documents, and entries that name no document."""
+    rng = np.random.default_rng(100 * Tq + nq)
+    pg, docs = _filled(rng, rng.integers(0, 40, 90), "bf16")
+    q = units(rng, nq * Tq).reshape(nq, Tq, 128)
+    Q = tensor(q)
+    ids = rng.integers(-3, 93, 330).astype(np.int32)
+    one = torch.from_numpy(ids).cuda()
+    each = one.expand(nq, 330).contiguous()
+    say("score", Tq, nq)
+    got = pg.score(Q, one)
+    check_scores(torch.cat([got[:1], got[-1:]]), torch.cat([Q[:1], Q[-1:]]), docs, [ids] * 2, "first and last")
+    assert torch.equal(got, pg.score(Q, each))
+    Q[nq // 2, Tq // 2, 5:70] = 3000.0
+    Q[nq - 1, 0, 127] = float("nan")
+    mixed = pg.score(Q, one)
+    finite = [i for i in range(nq) if i not in (nq // 2, nq - 1)]
+    assert torch.equal(mixed[finite], got[finite])
+    if nq > 2:
+        check_scores(mixed[nq // 2:nq // 2 + 1], Q[nq // 2:nq // 2 + 1], docs, [ids], "large values")
+    own = pg.score(Q, each)
+    assert torch.equal(mixed.nan_to_num(nan=9e9), own.nan_to_num(nan=9e9))
+
+
+@pytest.mark.parametrize("Tq", [1, 3, 8, 11, 32])
+def test_a_long_list_that_short_queries_share(Tq):
+    """Waves that take 64 entries each."""
+    rng = np.random.default_rng(Tq)
+    pg, docs = _filled(rng, rng.integers(0, 20, 300), "bf16")
+    Q = tensor(units(rng, 70 * Tq), "bf16").view(70, Tq, 128)
+    ids = torch.from_numpy(rng.integers(-3, 310, 140_000).astype(np.int32)).cuda()
+    say("score", Tq)
+    all_docs = torch.cat([pg.score(Q[i:i + 1]) for i in range(70)])
+    want = torch.where((ids >= 0) & (ids < 300), all_docs[:, ids.clamp(0, 299).long()], -float("inf"))
+    assert torch.equal(pg.score(Q, ids), want)
+
+
 def test_queries_as_views():
     """Queries that are strided, transposed or not 16-byte aligned, and repeated documents in a read."""
     rng = np.random.default_rng(18)
@@ -422,7 +462,7 @@ def test_score_in_a_graph():
 
 
 def test_more_queries_than_one_launch_takes():
-    """300,000 documents of one token: a launch takes 1,786 queries."""
+    """300,000 documents of one token: a launch takes 1,786 queries with a list each, and as many groups of them."""
     rng = np.random.default_rng(19)
     n, nq = 300_000, 1790
     X = tensor(units(rng, 5000), "bf16").repeat(n // 5000, 1)
@@ -437,6 +477,11 @@ def test_more_queries_than_one_launch_takes():
     assert torch.equal(own, got.flip(1))
     v = mx_values(host(X[:5000]))
     check_scores(got[:2, :5000], Q[:2], [t[None] for t in v], [range(5000)] * 2)
+    del got, own
+    Q = tensor(units(rng, 3575 * 17), "bf16").view(3575, 17, 128)
+    got = pg.score(Q)  # two queries a group
+    for q in (0, 3571, 3572, 3574):
+        assert torch.equal(got[q], pg.score(Q[q:q + 1])[0]), q
 
 
 def test_two_host_threads():
