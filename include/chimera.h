@@ -504,10 +504,11 @@ int chimera_pages_copy(chimera_pages *src, const int64_t *src_ids, chimera_pages
  * when no document holds it. */
 int chimera_pages_drop(chimera_pages *pg, const int64_t *doc_ids, int64_t n, void *hip_stream);
 
-/* out device [sum of lengths][128], CHIMERA_F32 or CHIMERA_BF16 (both hold every
- * value exactly), 16-byte aligned: the documents' values, one document behind
- * the other (repeats are allowed). */
-int chimera_pages_read(chimera_pages *pg, const int64_t *doc_ids, int64_t n, void *out, int dtype, void *hip_stream);
+/* out device [rows][128], CHIMERA_F32 or CHIMERA_BF16 (both hold every value
+ * exactly), 16-byte aligned: the documents' values, one document behind the
+ * other (repeats are allowed).  E_INVAL if they have more than `rows` tokens. */
+int chimera_pages_read(chimera_pages *pg, const int64_t *doc_ids, int64_t n, void *out, int64_t rows, int dtype,
+                       void *hip_stream);
 
 /* scores device [nq][n] float32: score(i, V) = sum_j max_{t in V} <Q_ij, v_t>
  * over the stored values v of document V = doc_ids[i * ld + c].

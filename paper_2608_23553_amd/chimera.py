@@ -93,7 +93,7 @@ def lib():
         "chimera_pages_fork": ([P, P, P, P, I64, P], INT),
         "chimera_pages_copy": ([P, P, P, P, P, P, I64, P], INT),
         "chimera_pages_drop": ([P, P, I64, P], INT),
-        "chimera_pages_read": ([P, P, I64, P, INT, P], INT),
+        "chimera_pages_read": ([P, P, I64, P, I64, INT, P], INT),
         "chimera_pages_score": ([P, P, INT, I64, I32, I32, P, I64, I64, P, P], INT),
         "chimera_search_pages": ([P, P, P, INT, I64, I32, I32, I32, I32, I32, P, P, P], INT),
         "chimera_search_collab_rabitq": ([P, P, INT, I64, I32, I32, I32, I32, I32, I32, I32, P, P, P, I32, P],
@@ -657,7 +657,7 @@ class Pages:
                 out = torch.empty((rows, 128), dtype=dtype or torch.bfloat16, device=self.device)
         elif tuple(out.shape) != (rows, 128) or not out.is_contiguous() or (dtype is not None and out.dtype != dtype):
             raise ValueError(f"out must be a contiguous tensor [{rows}, 128]{'' if dtype is None else f' of {dtype}'}")
-        _check(self._lib.chimera_pages_read(self._h, _at(a), a.size, out.data_ptr(), self._type(out, "out"),
+        _check(self._lib.chimera_pages_read(self._h, _at(a), a.size, out.data_ptr(), rows, self._type(out, "out"),
                                             self._stream(stream)))
         return out
 

@@ -369,7 +369,8 @@ int chimera_pages_drop(chimera_pages *pg, const int64_t *doc_ids, int64_t n, voi
   });
 }
 
-int chimera_pages_read(chimera_pages *pg, const int64_t *doc_ids, int64_t n, void *out, int dtype, void *hip_stream) {
+int chimera_pages_read(chimera_pages *pg, const int64_t *doc_ids, int64_t n, void *out, int64_t rows, int dtype,
+                       void *hip_stream) {
   if (int rc = check_list(pg, doc_ids, n, "read")) return rc;
   if (dtype != CHIMERA_F32 && dtype != CHIMERA_BF16) return fail(CHIMERA_E_INVAL, "dtype must be F32 or BF16");
   if ((uintptr_t)out % 16) return fail(CHIMERA_E_INVAL, "read: out must be 16-byte aligned");
@@ -379,9 +380,11 @@ int chimera_pages_read(chimera_pages *pg, const int64_t *doc_ids, int64_t n, voi
   DeviceGuard dg(pg->device);
   if (!dg.ok) return fail(CHIMERA_E_DEVICE, "cannot select device %d", pg->device);
   return guarded([&]() -> int {
-    int64_t at = 0, items = 0, rows = 0;
-    if (BookError e = pg->book.check_read(doc_ids, n, &at, &items, &rows); e != BookError::none)
+    int64_t at = 0, items = 0, total = 0;
+    if (BookError e = pg->book.check_read(doc_ids, n, &at, &items, &total); e != BookError::none)
       return book_fail(e, "read", doc_ids, at);
+    if (total > rows)
+      return fail(CHIMERA_E_INVAL, "read: %lld tokens, out has %lld rows", (long long)total, (long long)rows);
     if (items == 0) return CHIMERA_OK;
     if (!out) return fail(CHIMERA_E_INVAL, "null output pointer");
     if (items > kPagesMaxItems) return fail(CHIMERA_E_UNSUPPORTED, "read: too many tokens in one call");

@@ -601,7 +601,13 @@ def test_refusals_leave_everything_as_it_was():
     assert L.chimera_pages_score(h, Q.data_ptr(), 0, 1, 32, 128, sc.data_ptr(), 5, 4, sc.data_ptr(), s) == bad
     assert L.chimera_pages_score(h, Q.data_ptr(), 0, 1, 32, 128, None, 2**28 + 1, 0, sc.data_ptr(),
                                  s) == chimera.E_UNSUPPORTED
-    assert L.chimera_pages_read(h, one, 1, X.data_ptr() + 8, 0, s) == bad
+    assert L.chimera_pages_read(h, one, 1, X.data_ptr() + 8, 64, 0, s) == bad
+    two = (ctypes.c_int64 * 2)(0, 1)
+    held = torch.full((53, 128), 7.0, device="cuda")
+    for rows in (52, 0, -1):  # as after another thread's append between the lengths and the read
+        assert L.chimera_pages_read(h, two, 2, held.data_ptr(), rows, 0, s) == bad
+    torch.cuda.synchronize()
+    assert torch.all(held == 7.0)
     torch.cuda.synchronize()
     assert torch.all(sc == 7.0) and pg.info() == info
     same(pg.read([0, 1, 2, 3, 4]), np.concatenate(docs))

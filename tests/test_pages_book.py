@@ -30,7 +30,7 @@ def test_null_arguments_are_rejected_without_gpu():
     assert L.chimera_pages_fork(None, one, one, len1, 1, None) == bad
     assert L.chimera_pages_copy(None, one, None, one, len1, None, 1, None) == bad
     assert L.chimera_pages_drop(None, one, 1, None) == bad
-    assert L.chimera_pages_read(None, one, 1, None, 0, None) == bad
+    assert L.chimera_pages_read(None, one, 1, None, 0, 0, None) == bad
     assert L.chimera_pages_score(None, None, 0, 1, 32, 128, None, 1, 0, None, None) == bad
     assert L.chimera_search_pages(None, None, None, 0, 1, 32, 128, 2, 256, 10, None, None, None) == bad
     assert b"null index" in L.chimera_last_error()
