@@ -663,7 +663,7 @@ class Pages:
 
     def score(self, Q, ids=None, out=None, stream=None):
         """Scores float32 [nq, n] of queries Q [nq, Tq, 128] with stored documents (chimera_pages_score): ids int32 on
-        the GPU, [nq, n] a list for each query or [n] one for all; None: every document 0 .. ndocs - 1."""
+        the GPU, [nq, n] a list for each query or [n] (also expanded) one for all; None: every document 0 .. ndocs - 1."""
         import torch
         dt = self._type(Q, "Q")
         if Q.dim() != 3:
@@ -680,7 +680,7 @@ class Pages:
             if k == 2 and ids.shape[0] != nq:
                 raise ValueError(f"ids must be [{nq}, n], got {list(ids.shape)}")
             n = ids.shape[-1]
-            if ids.stride(-1) != 1 or (k == 2 and nq > 1 and ids.stride(0) < n):
+            if ids.stride(-1) != 1 or (k == 2 and nq > 1 and 0 < ids.stride(0) < n):
                 with _on(stream):
                     ids = ids.contiguous()
             ld = ids.stride(0) if k == 2 and nq > 1 else 0

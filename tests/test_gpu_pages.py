@@ -180,7 +180,9 @@ def test_short_queries_that_share_a_list(Tq, nq):
     say("score", Tq, nq)
     got = pg.score(Q, one)
     check_scores(torch.cat([got[:1], got[-1:]]), torch.cat([Q[:1], Q[-1:]]), docs, [ids] * 2, "first and last")
-    assert torch.equal(got, pg.score(Q, each))
+    assert torch.equal(got, pg.score(Q, each)) and torch.equal(got, pg.score(Q, one.expand(nq, 330)))
+    overlapping = one.as_strided((nq, 100), (1, 1))
+    assert torch.equal(pg.score(Q, overlapping)[-1], got[-1, nq - 1:nq + 99])
     Q[nq // 2, Tq // 2, 5:70] = 3000.0
     Q[nq - 1, 0, 127] = float("nan")
     mixed = pg.score(Q, one)
@@ -473,8 +475,9 @@ def test_more_queries_than_one_launch_takes():
     for q in (0, 1, 1785, 1786, 1789):
         assert torch.equal(got[q], pg.score(Q[q:q + 1])[0]), q
     ids = torch.arange(n - 1, -1, -1, dtype=torch.int32, device="cuda").expand(nq, n)
-    own = pg.score(Q, ids)
+    own = pg.score(Q, ids.contiguous())
     assert torch.equal(own, got.flip(1))
+    assert torch.equal(pg.score(Q, ids), own)  # expanded: one list
     v = mx_values(host(X[:5000]))
     check_scores(got[:2, :5000], Q[:2], [t[None] for t in v], [range(5000)] * 2)
     del got, own
