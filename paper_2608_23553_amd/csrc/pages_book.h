@@ -229,6 +229,10 @@ struct PageBook {
     const bool same = &to == this;
     *items = *pages = *npos = *turns = 0;
     *in_place = false;
+    // there are sum lens positions: as many as a document's length says only
+    // where no other one is below zero, and else none is read (the call is refused)
+    int32_t least = 0;
+    for (int64_t i = 0; pos && i < n; ++i) least = lens[i] < least ? lens[i] : least;
     for (int64_t i = 0; i < n; ++i) {
       *at = i;
       if (src[i] < 0 || src[i] >= ndocs) return BookError::id;
@@ -238,7 +242,7 @@ struct PageBook {
       const int32_t have = len[src[i]], l = lens ? lens[i] : have;
       if (l < 0 || l > have) return BookError::length;
       if (l > to.max_len) return BookError::too_long;
-      if (pos && l) {
+      if (pos && l && least == 0) {
         const int32_t *q = pos + *npos;
         if (q[0] < 0 || q[l - 1] >= have) return BookError::position;
         *turns += *npos && q[0] <= q[-1];

@@ -58,3 +58,11 @@ def test_ids_and_lengths_are_whole_numbers(bad):
     with pytest.raises(ValueError):
         chimera._counts([1, 2], 1, "lens")
     assert chimera._ids([]).dtype == np.int64 and chimera._counts([], 0, "lens").dtype == np.int32
+
+
+def test_lengths_of_a_copy_are_checked_before_its_positions_are_read(tmp_path):
+    exe = str(tmp_path / "lengths")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-D_GLIBCXX_ASSERTIONS", "-Wall", "-o", exe,
+                           os.path.join(HERE, "pages_copy_lengths.cpp")])
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout
