@@ -443,10 +443,11 @@ int chimera_search_collab_rabitq(chimera_index *idx, const void *Q, int q_dtype,
  *    their streams.  Tensors handed in (X, Q, the score's doc_ids) are read and
  *    outputs written on hip_stream alone.  Only chimera_pages_score can be
  *    captured into a graph (the others return E_UNSUPPORTED: their bookkeeping
- *    would happen once); a captured score and its replays are not ordered by
+ *    would happen once; so does chimera_search_pages, whose scratch is handed
+ *    from call to call); a captured score and its replays are not ordered by
  *    the library: the caller keeps them apart from calls that change the
  *    store and run on other streams.  A replay scores the documents as they
- *    are when it runs.  A search (chimera_search_pages) cannot be captured.
+ *    are when it runs.
  *  - Concurrent host calls on one store return E_BUSY; info_get and lengths
  *    must not overlap a call that changes the store.  After E_DEVICE the store
  *    must be freed.

@@ -777,8 +777,10 @@ int chimera_search_pages(chimera_index *idx, chimera_pages *pg, const void *Q, i
   DeviceGuard dg(pg->device);
   if (!dg.ok) return fail(CHIMERA_E_DEVICE, "cannot select device %d", pg->device);
   hipStream_t s = (hipStream_t)hip_stream;
-  if (nq > 0)
+  if (nq > 0) {
+    if (int rc = pages_not_captured(s, "search from pages", "the index's scratch is handed from call to call")) return rc;
     if (int rc = pages_order_before(pg, s)) return rc;
+  }
   int rc = search_common(idx, Q, q_dtype, nq, Tq, d, nprobe, ncand, k, CHIMERA_REFINE_CENTROID, ids, scores, hip_stream,
                          false, false, &pg->view);
   // also after an error: some of the search may be queued

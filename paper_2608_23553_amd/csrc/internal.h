@@ -265,6 +265,8 @@ void launch_pages_score(const void *Q, int q_dtype, int64_t nq, int Tq, int q_st
                         const int32_t *n_valid, int64_t n, const PagesView &pg, void *out, bool keys, hipStream_t s);
 // Results [n] whose key is the lowest (documents without tokens in the store) become (-1, -inf).
 void launch_pages_unscored(int32_t *ids, float *scores, int64_t n, hipStream_t s);
+// E_UNSUPPORTED, with the reason `why`, where s is being captured into a graph.
+int pages_not_captured(hipStream_t s, const char *call, const char *why);
 // Work on s comes after every earlier call on the store; later calls after the work on s.
 int pages_order_before(chimera_pages *pg, hipStream_t s);
 int pages_order_after(chimera_pages *pg, hipStream_t s);

@@ -21,6 +21,11 @@ static bool capturing(hipStream_t s) {
   return st != hipStreamCaptureStatusNone;
 }
 
+int pages_not_captured(hipStream_t s, const char *call, const char *why) {
+  if (capturing(s)) return fail(CHIMERA_E_UNSUPPORTED, "%s: cannot be captured into a graph (%s)", call, why);
+  return CHIMERA_OK;
+}
+
 int pages_order_before(chimera_pages *pg, hipStream_t s) {
   if (pg->on_null && s == nullptr) return CHIMERA_OK;
   if (pg->on_null) {
@@ -124,9 +129,7 @@ static int check_list(const chimera_pages *pg, const void *ids, int64_t n, const
   return CHIMERA_OK;
 }
 static int check_stream(hipStream_t s, const char *call) {
-  if (capturing(s))
-    return fail(CHIMERA_E_UNSUPPORTED, "%s: cannot be captured into a graph (its host bookkeeping happens once)", call);
-  return CHIMERA_OK;
+  return pages_not_captured(s, call, "its host bookkeeping happens once");
 }
 
 }  // namespace chimera
