@@ -254,6 +254,13 @@ def _stream_ptr(stream) -> ctypes.c_void_p:
     return ctypes.c_void_p(stream.cuda_stream)
 
 
+def _on(stream):
+    """Where a call's own tensors are made: on its stream, so that copies are in order with the call and the memory
+    is not given away while it runs."""
+    import torch
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 def _q_args(Q):
     import torch
     if not Q.is_cuda:
@@ -308,10 +315,11 @@ class Index:
         _check(lib().chimera_index_compact(self._h))
         self._info = self.info()
 
-    def _q(self, Q):
+    def _q(self, Q, stream):
         """Q as the library takes it, on the index's own GPU (the library
         receives a bare device pointer and cannot check that)."""
-        Q, dt = _q_args(Q)
+        with _on(stream):
+            Q, dt = _q_args(Q)
         if Q.device.index != self._info["device"]:
             raise ValueError(f"Q is on {Q.device}, the index on cuda:{self._info['device']}")
         return Q, dt
@@ -321,12 +329,13 @@ class Index:
         import torch
         return torch.device("cuda", self._info["device"])
 
-    def _results(self, Q, nq, k, out):
+    def _results(self, Q, nq, k, out, stream):
         """The tensors of a search's results: new ones, or out's, checked."""
         import torch
         if out is None:
-            return (torch.empty((nq, k), dtype=torch.int32, device=Q.device),
-                    torch.empty((nq, k), dtype=torch.float32, device=Q.device))
+            with _on(stream):
+                return (torch.empty((nq, k), dtype=torch.int32, device=Q.device),
+                        torch.empty((nq, k), dtype=torch.float32, device=Q.device))
         ids, scores = out
         for t, dtype, name in ((ids, torch.int32, "ids"), (scores, torch.float32, "scores")):
             if tuple(t.shape) != (nq, k) or t.dtype != dtype or t.device != Q.device or not t.is_contiguous():
@@ -337,9 +346,9 @@ class Index:
         """Top-k (ids int32 [nq,k], scores float32 [nq,k]) for queries Q [nq,Tq,d].
         refine: REFINE_CENTROID (chimera_search) or REFINE_TOKEN
         (chimera_search_refine)."""
-        Q, dt = self._q(Q)
+        Q, dt = self._q(Q, stream)
         nq, Tq, d = Q.shape
-        ids, scores = self._results(Q, nq, k, out)
+        ids, scores = self._results(Q, nq, k, out, stream)
         if refine == REFINE_CENTROID:
             _check(lib().chimera_search(self._h, ctypes.c_void_p(Q.data_ptr()), dt, nq, Tq, d, nprobe, ncand, k,
                                         ctypes.c_void_p(ids.data_ptr()), ctypes.c_void_p(scores.data_ptr()),
@@ -353,11 +362,12 @@ class Index:
     def search_rabitq(self, Q, nprobe: int, ncand: int, k: int, out=None, stream=None):
         """chimera_search_rabitq: step 4 scored from the RaBitQ 1-bit codes."""
         import torch
-        Q, dt = self._q(Q)
+        Q, dt = self._q(Q, stream)
         nq, Tq, d = Q.shape
         if out is None:
-            ids = torch.empty((nq, k), dtype=torch.int32, device=Q.device)
-            scores = torch.empty((nq, k), dtype=torch.float32, device=Q.device)
+            with _on(stream):
+                ids = torch.empty((nq, k), dtype=torch.int32, device=Q.device)
+                scores = torch.empty((nq, k), dtype=torch.float32, device=Q.device)
         else:
             ids, scores = out
         _check(lib().chimera_search_rabitq(self._h, ctypes.c_void_p(Q.data_ptr()), dt, nq, Tq, d, nprobe, ncand, k,
@@ -367,9 +377,9 @@ class Index:
 
     def search_pages(self, pages: "Pages", Q, nprobe: int, ncand: int, k: int, out=None, stream=None):
         """chimera_search_pages: step 4 scored from a paged store's documents of the same ids."""
-        Q, dt = self._q(Q)
+        Q, dt = self._q(Q, stream)
         nq, Tq, d = Q.shape
-        ids, scores = self._results(Q, nq, k, out)
+        ids, scores = self._results(Q, nq, k, out, stream)
         _check(lib().chimera_search_pages(self._h, pages._h, Q.data_ptr(), dt, nq, Tq, d, nprobe, ncand, k,
                                           ids.data_ptr(), scores.data_ptr(), _stream_ptr(stream)))
         return ids, scores
@@ -401,7 +411,7 @@ class Index:
                       stream=None):
         """CPU-GPU collaborative scoring (chimera_search_collab): host numpy
         (ids int32 [nq,k], scores float32 [nq,k], n_full int32 [nq])."""
-        Q, dt = self._q(Q)
+        Q, dt = self._q(Q, stream)
         nq, Tq, d = Q.shape
         ids = np.empty((nq, k), dtype=np.int32)
         scores = np.empty((nq, k), dtype=np.float32)
@@ -415,7 +425,7 @@ class Index:
                              stream=None):
         """chimera_search_collab_rabitq: GPU 1-bit RaBitQ scores, host 4-bit
         RaBitQ scores (host numpy ids, scores, n_full)."""
-        Q, dt = self._q(Q)
+        Q, dt = self._q(Q, stream)
         nq, Tq, d = Q.shape
         ids = np.empty((nq, k), dtype=np.int32)
         scores = np.empty((nq, k), dtype=np.float32)
@@ -433,10 +443,11 @@ class Index:
 
     def probe(self, Q, nprobe: int, stream=None):
         import torch
-        Q, dt = self._q(Q)
+        Q, dt = self._q(Q, stream)
         nq, Tq, d = Q.shape
-        ids = torch.empty((nq, Tq, nprobe), dtype=torch.int32, device=Q.device)
-        keys = torch.empty((nq, Tq, nprobe), dtype=torch.int32, device=Q.device)
+        with _on(stream):
+            ids = torch.empty((nq, Tq, nprobe), dtype=torch.int32, device=Q.device)
+            keys = torch.empty((nq, Tq, nprobe), dtype=torch.int32, device=Q.device)
         _check(lib().chimera_probe(self._h, ctypes.c_void_p(Q.data_ptr()), dt, nq, Tq, d, nprobe,
                                    ctypes.c_void_p(ids.data_ptr()), ctypes.c_void_p(keys.data_ptr()),
                                    _stream_ptr(stream)))
@@ -444,12 +455,13 @@ class Index:
 
     def candidates(self, Q, nprobe: int, capacity: int | None = None, stream=None):
         import torch
-        Q, dt = self._q(Q)
+        Q, dt = self._q(Q, stream)
         nq, Tq, d = Q.shape
         if capacity is None:
             capacity = nq * self._info["ndocs"]
-        offsets = torch.empty(nq + 1, dtype=torch.int64, device=Q.device)
-        doc_ids = torch.empty(max(capacity, 1), dtype=torch.int32, device=Q.device)
+        with _on(stream):
+            offsets = torch.empty(nq + 1, dtype=torch.int64, device=Q.device)
+            doc_ids = torch.empty(max(capacity, 1), dtype=torch.int32, device=Q.device)
         _check(lib().chimera_candidates(self._h, ctypes.c_void_p(Q.data_ptr()), dt, nq, Tq, d, nprobe,
                                         ctypes.c_void_p(offsets.data_ptr()), ctypes.c_void_p(doc_ids.data_ptr()),
                                         capacity, _stream_ptr(stream)))
@@ -457,12 +469,13 @@ class Index:
 
     def prune(self, Q, nprobe: int, ncand: int, stream=None, refine: int = REFINE_CENTROID):
         import torch
-        Q, dt = self._q(Q)
+        Q, dt = self._q(Q, stream)
         nq, Tq, d = Q.shape
         nc = min(ncand, self._info["ndocs"])
-        cand = torch.empty((nq, nc), dtype=torch.int32, device=Q.device)
-        keys = torch.empty((nq, nc), dtype=torch.int32, device=Q.device)
-        nval = torch.empty(nq, dtype=torch.int32, device=Q.device)
+        with _on(stream):
+            cand = torch.empty((nq, nc), dtype=torch.int32, device=Q.device)
+            keys = torch.empty((nq, nc), dtype=torch.int32, device=Q.device)
+            nval = torch.empty(nq, dtype=torch.int32, device=Q.device)
         if refine == REFINE_CENTROID:
             _check(lib().chimera_prune(self._h, ctypes.c_void_p(Q.data_ptr()), dt, nq, Tq, d, nprobe, ncand,
                                        ctypes.c_void_p(cand.data_ptr()), ctypes.c_void_p(keys.data_ptr()),
@@ -488,13 +501,6 @@ class Index:
 def _aligned(t):
     """t, or a copy where its first value is not 16-byte aligned, as the library asks."""
     return t if t.data_ptr() % 16 == 0 else t.clone()
-
-
-def _on(stream):
-    """Where a call's own tensors are made: on its stream, so that copies are in order with the call and the memory
-    is not given away while it runs."""
-    import torch
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
 def _ids(ids) -> np.ndarray:

@@ -5,7 +5,9 @@ import numpy as np
 import pytest
 import torch
 
+import synth
 from paper_2608_23553_amd import ChimeraError, Pages, chimera
+from util_build import product_builder
 from util_gpu import q_tensor, say, setup
 from util_pages import check_scores, host, mx_values, same, tensor, units
 
@@ -58,3 +60,63 @@ def test_a_search_in_a_capture_is_refused(before):
             same(pg.read([5]), v[:7])
     pg.drop([3, 4, 5])
     assert pg.info()["ntokens"] == 0
+
+
+# ------------------------------------------------------------ streams
+def _later(Q):
+    """Q as a view that the library cannot take as it is."""
+    wide = torch.zeros(Q.shape[0], Q.shape[1], 2, Q.shape[2], dtype=Q.dtype, device="cuda")
+    wide[:, :, 0] = Q
+    return wide[:, :, 0]
+
+
+@pytest.mark.parametrize("call", ["search_pages", "search", "refine", "rabitq", "collab", "probe", "prune", "candidates"])
+def test_a_search_on_another_stream_than_the_current_one(call):
+    """Strided queries and new results of a call on a stream of its own, while the current stream has work to do and
+    takes memory as soon as the call returns: the same as on the current stream."""
+    w, c, kk, cl, oi, idx = setup("tiny")
+    if call in ("rabitq", "collab"):
+        signs = synth.rotation_signs(17) if call == "rabitq" else None
+        idx = product_builder(c, w.nbits, rabitq_signs=signs).upload(0)
+        if call == "collab":
+            idx.attach_fullbit(synth.k_to_bf16_bits(kk))
+    q, _ = c.queries(16, w.Tq, query_seed=41)
+    Q = q_tensor(q, "bf16")
+    pg = Pages(4000, 1000, 64)
+    lens = np.diff(c.doc_off).astype(np.int32)
+    pg.append(np.arange(len(lens)), torch.from_numpy(synth.k_to_f32(kk)).cuda(), lens)
+    args = (w.nprobe, w.ncand, 10)
+    f = {"search_pages": lambda Q, **k: idx.search_pages(pg, Q, *args, **k),
+         "search": lambda Q, **k: idx.search(Q, *args, **k),
+         "refine": lambda Q, **k: idx.search(Q, *args, refine=chimera.REFINE_TOKEN, **k),
+         "rabitq": lambda Q, **k: idx.search_rabitq(Q, *args, **k),
+         "collab": lambda Q, **k: idx.search_collab(Q, w.nprobe, w.ncand, 20, 2, 10, **k),
+         "probe": lambda Q, **k: idx.probe(Q, w.nprobe, **k),
+         "prune": lambda Q, **k: idx.prune(Q, w.nprobe, w.ncand, **k),
+         "candidates": lambda Q, **k: idx.candidates(Q, w.nprobe, **k)}[call]
+    want = f(Q)
+    view = _later(Q)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        say(call, "beside the current stream")
+        torch.cuda._sleep(20_000_000)
+        got = f(view, stream=side)
+        junk = [torch.full((n,), float("nan"), device="cuda") for n in (160, 16 * 32 * 64, 1 << 18) for _ in range(4)]
+        side.synchronize()
+        torch.cuda.synchronize()
+        for a, b in zip(_written(call, got), _written(call, want)):
+            assert type(a) is type(b) and a.shape == b.shape and bool((a == b).all()), call
+        del got, junk
+
+
+def _written(call, out):
+    """What a call writes of its outputs."""
+    if call == "candidates":
+        offsets, docs = out
+        return offsets, docs[:int(offsets[-1])]
+    if call == "prune":
+        cand, keys, n = out
+        here = torch.arange(cand.shape[1], device="cuda") < n[:, None]
+        return cand[here], keys[here], n
+    return out
