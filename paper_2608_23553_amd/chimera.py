@@ -247,13 +247,6 @@ def build_index(centroids_bf16: np.ndarray, nbits: int,
 
 
 # ----------------------------------------------------------------- index
-def _stream_ptr(stream) -> ctypes.c_void_p:
-    import torch
-    if stream is None:
-        stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream)
-
-
 def _on(stream):
     """Where a call's own tensors are made: on its stream, so that copies are in order with the call and the memory
     is not given away while it runs."""
@@ -329,6 +322,11 @@ class Index:
         import torch
         return torch.device("cuda", self._info["device"])
 
+    def _stream(self, stream) -> ctypes.c_void_p:
+        """A call's stream: None is the current one of the index's own GPU, which need not be the current GPU."""
+        import torch
+        return ctypes.c_void_p((torch.cuda.current_stream(self.device) if stream is None else stream).cuda_stream)
+
     def _results(self, Q, nq, k, out, stream):
         """The tensors of a search's results: new ones, or out's, checked."""
         import torch
@@ -352,11 +350,11 @@ class Index:
         if refine == REFINE_CENTROID:
             _check(lib().chimera_search(self._h, ctypes.c_void_p(Q.data_ptr()), dt, nq, Tq, d, nprobe, ncand, k,
                                         ctypes.c_void_p(ids.data_ptr()), ctypes.c_void_p(scores.data_ptr()),
-                                        _stream_ptr(stream)))
+                                        self._stream(stream)))
         else:
             _check(lib().chimera_search_refine(self._h, ctypes.c_void_p(Q.data_ptr()), dt, nq, Tq, d, nprobe, ncand,
                                                k, refine, ctypes.c_void_p(ids.data_ptr()),
-                                               ctypes.c_void_p(scores.data_ptr()), _stream_ptr(stream)))
+                                               ctypes.c_void_p(scores.data_ptr()), self._stream(stream)))
         return ids, scores
 
     def search_rabitq(self, Q, nprobe: int, ncand: int, k: int, out=None, stream=None):
@@ -372,7 +370,7 @@ class Index:
             ids, scores = out
         _check(lib().chimera_search_rabitq(self._h, ctypes.c_void_p(Q.data_ptr()), dt, nq, Tq, d, nprobe, ncand, k,
                                            ctypes.c_void_p(ids.data_ptr()), ctypes.c_void_p(scores.data_ptr()),
-                                           _stream_ptr(stream)))
+                                           self._stream(stream)))
         return ids, scores
 
     def search_pages(self, pages: "Pages", Q, nprobe: int, ncand: int, k: int, out=None, stream=None):
@@ -381,7 +379,7 @@ class Index:
         nq, Tq, d = Q.shape
         ids, scores = self._results(Q, nq, k, out, stream)
         _check(lib().chimera_search_pages(self._h, pages._h, Q.data_ptr(), dt, nq, Tq, d, nprobe, ncand, k,
-                                          ids.data_ptr(), scores.data_ptr(), _stream_ptr(stream)))
+                                          ids.data_ptr(), scores.data_ptr(), self._stream(stream)))
         return ids, scores
 
     def attach_fullbit(self, tokens_bf16):
@@ -418,7 +416,7 @@ class Index:
         n_full = np.empty(nq, dtype=np.int32)
         _check(lib().chimera_search_collab(self._h, ctypes.c_void_p(Q.data_ptr()), dt, nq, Tq, d, nprobe, ncand, kfb,
                                            chunks, k, _np(ids), _np(scores), _np(n_full), nthreads,
-                                           _stream_ptr(stream)))
+                                           self._stream(stream)))
         return ids, scores, n_full
 
     def search_collab_rabitq(self, Q, nprobe: int, ncand: int, kfb: int, chunks: int, k: int, nthreads: int = 0,
@@ -432,7 +430,7 @@ class Index:
         n_full = np.empty(nq, dtype=np.int32)
         _check(lib().chimera_search_collab_rabitq(self._h, ctypes.c_void_p(Q.data_ptr()), dt, nq, Tq, d, nprobe,
                                                   ncand, kfb, chunks, k, _np(ids), _np(scores), _np(n_full),
-                                                  nthreads, _stream_ptr(stream)))
+                                                  nthreads, self._stream(stream)))
         return ids, scores, n_full
 
     def search_raw(self, q_ptr: int, q_dtype: int, nq: int, Tq: int, d: int, nprobe: int, ncand: int, k: int,
@@ -450,7 +448,7 @@ class Index:
             keys = torch.empty((nq, Tq, nprobe), dtype=torch.int32, device=Q.device)
         _check(lib().chimera_probe(self._h, ctypes.c_void_p(Q.data_ptr()), dt, nq, Tq, d, nprobe,
                                    ctypes.c_void_p(ids.data_ptr()), ctypes.c_void_p(keys.data_ptr()),
-                                   _stream_ptr(stream)))
+                                   self._stream(stream)))
         return ids, keys
 
     def candidates(self, Q, nprobe: int, capacity: int | None = None, stream=None):
@@ -464,7 +462,7 @@ class Index:
             doc_ids = torch.empty(max(capacity, 1), dtype=torch.int32, device=Q.device)
         _check(lib().chimera_candidates(self._h, ctypes.c_void_p(Q.data_ptr()), dt, nq, Tq, d, nprobe,
                                         ctypes.c_void_p(offsets.data_ptr()), ctypes.c_void_p(doc_ids.data_ptr()),
-                                        capacity, _stream_ptr(stream)))
+                                        capacity, self._stream(stream)))
         return offsets, doc_ids
 
     def prune(self, Q, nprobe: int, ncand: int, stream=None, refine: int = REFINE_CENTROID):
@@ -479,12 +477,12 @@ class Index:
         if refine == REFINE_CENTROID:
             _check(lib().chimera_prune(self._h, ctypes.c_void_p(Q.data_ptr()), dt, nq, Tq, d, nprobe, ncand,
                                        ctypes.c_void_p(cand.data_ptr()), ctypes.c_void_p(keys.data_ptr()),
-                                       ctypes.c_void_p(nval.data_ptr()), _stream_ptr(stream)))
+                                       ctypes.c_void_p(nval.data_ptr()), self._stream(stream)))
         else:
             _check(lib().chimera_prune_refine(self._h, ctypes.c_void_p(Q.data_ptr()), dt, nq, Tq, d, nprobe, ncand,
                                               refine, ctypes.c_void_p(cand.data_ptr()),
                                               ctypes.c_void_p(keys.data_ptr()), ctypes.c_void_p(nval.data_ptr()),
-                                              _stream_ptr(stream)))
+                                              self._stream(stream)))
         return cand, keys, nval
 
     def stage_times(self) -> np.ndarray:
