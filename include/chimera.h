@@ -510,6 +510,12 @@ int chimera_pages_drop(chimera_pages *pg, const int64_t *doc_ids, int64_t n, voi
  * other (repeats are allowed).  E_INVAL if they have more than `rows` tokens. */
 int chimera_pages_read(chimera_pages *pg, const int64_t *doc_ids, int64_t n, void *out, int64_t rows, int dtype,
                        void *hip_stream);
+/* The same for an out that the documents fill: *total (not NULL) becomes the
+ * number of their tokens, and unless that is `rows` the call is E_INVAL and
+ * nothing is read (another thread changed the store since the caller counted).
+ * rows < 0: only *total. */
+int chimera_pages_read_all(chimera_pages *pg, const int64_t *doc_ids, int64_t n, void *out, int64_t rows, int dtype,
+                           int64_t *total, void *hip_stream);
 
 /* scores device [nq][n] float32: score(i, V) = sum_j max_{t in V} <Q_ij, v_t>
  * over the stored values v of document V = doc_ids[i * ld + c].

@@ -94,6 +94,7 @@ def lib():
         "chimera_pages_copy": ([P, P, P, P, P, P, I64, P], INT),
         "chimera_pages_drop": ([P, P, I64, P], INT),
         "chimera_pages_read": ([P, P, I64, P, I64, INT, P], INT),
+        "chimera_pages_read_all": ([P, P, I64, P, I64, INT, P, P], INT),
         "chimera_pages_score": ([P, P, INT, I64, I32, I32, P, I64, I64, P, P], INT),
         "chimera_search_pages": ([P, P, P, INT, I64, I32, I32, I32, I32, I32, P, P, P], INT),
         "chimera_search_collab_rabitq": ([P, P, INT, I64, I32, I32, I32, I32, I32, I32, I32, P, P, P, I32, P],
@@ -650,19 +651,19 @@ class Pages:
 
     def read(self, ids, dtype=None, out=None, stream=None):
         """The stored values of documents, one behind the other: [sum of lengths, 128], bfloat16 unless dtype says
-        float32 (chimera_pages_read)."""
+        float32 (chimera_pages_read_all).  ChimeraError where another thread changes the documents' lengths meanwhile."""
         import torch
         a = _ids(ids)
         total = ctypes.c_int64()
-        _check(self._lib.chimera_pages_lengths(self._h, _at(a), a.size, None, ctypes.byref(total)))
+        _check(self._lib.chimera_pages_read_all(self._h, _at(a), a.size, None, -1, BF16, ctypes.byref(total), None))
         rows = total.value
         if out is None:
             with _on(stream):
                 out = torch.empty((rows, 128), dtype=dtype or torch.bfloat16, device=self.device)
         elif tuple(out.shape) != (rows, 128) or not out.is_contiguous() or (dtype is not None and out.dtype != dtype):
             raise ValueError(f"out must be a contiguous tensor [{rows}, 128]{'' if dtype is None else f' of {dtype}'}")
-        _check(self._lib.chimera_pages_read(self._h, _at(a), a.size, out.data_ptr(), rows, self._type(out, "out"),
-                                            self._stream(stream)))
+        _check(self._lib.chimera_pages_read_all(self._h, _at(a), a.size, out.data_ptr(), rows, self._type(out, "out"),
+                                                ctypes.byref(total), self._stream(stream)))
         return out
 
     def score(self, Q, ids=None, out=None, stream=None):

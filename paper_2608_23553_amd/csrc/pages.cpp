@@ -132,6 +132,41 @@ static int check_stream(hipStream_t s, const char *call) {
   return pages_not_captured(s, call, "its host bookkeeping happens once");
 }
 
+// exact: the documents' tokens, which have to be as many as rows (below 0: nothing
+// is read); null: at most as many.
+static int read_common(chimera_pages *pg, const int64_t *doc_ids, int64_t n, void *out, int64_t rows, int dtype,
+                       int64_t *exact, void *hip_stream) {
+  if (int rc = check_list(pg, doc_ids, n, "read")) return rc;
+  if (dtype != CHIMERA_F32 && dtype != CHIMERA_BF16) return fail(CHIMERA_E_INVAL, "dtype must be F32 or BF16");
+  if ((uintptr_t)out % 16) return fail(CHIMERA_E_INVAL, "read: out must be 16-byte aligned");
+  hipStream_t s = (hipStream_t)hip_stream;
+  BusyGuard<chimera_pages> bg(pg);
+  if (!bg.ok) return fail(CHIMERA_E_BUSY, "pages in use by another thread");
+  DeviceGuard dg(pg->device);
+  if (!dg.ok) return fail(CHIMERA_E_DEVICE, "cannot select device %d", pg->device);
+  return guarded([&]() -> int {
+    int64_t at = 0, items = 0, total = 0;
+    if (BookError e = pg->book.check_read(doc_ids, n, &at, &items, &total); e != BookError::none)
+      return book_fail(e, "read", doc_ids, at);
+    if (exact) *exact = total;
+    if (exact && rows < 0) return CHIMERA_OK;
+    if (total > rows || (exact && total < rows))
+      return fail(CHIMERA_E_INVAL, "read: %lld tokens, out has %lld rows", (long long)total, (long long)rows);
+    if (items == 0) return CHIMERA_OK;
+    if (!out) return fail(CHIMERA_E_INVAL, "null output pointer");
+    if (items > kPagesMaxItems) return fail(CHIMERA_E_UNSUPPORTED, "read: too many tokens in one call");
+    if (int rc = check_stream(s, "read")) return rc;
+    char *plan = nullptr;
+    if (int rc = pages_order_before(pg, s)) return rc;
+    if (int rc = ring_take(pg, (size_t)items * sizeof(PageItem), s, &plan)) return rc;
+    pg->book.plan_read(doc_ids, n, (PageItem *)plan);
+    const PageItem *it = (const PageItem *)plan_for_device(pg, plan, (size_t)items * sizeof(PageItem), s);
+    launch_pages_read(it, items, pg->view.pool, pg->view.table, pg->view.stride, out, dtype, s);
+    CHIMERA_HIP(hipGetLastError());
+    return pages_order_after(pg, s);
+  });
+}
+
 }  // namespace chimera
 
 using namespace chimera;
@@ -374,33 +409,13 @@ int chimera_pages_drop(chimera_pages *pg, const int64_t *doc_ids, int64_t n, voi
 
 int chimera_pages_read(chimera_pages *pg, const int64_t *doc_ids, int64_t n, void *out, int64_t rows, int dtype,
                        void *hip_stream) {
-  if (int rc = check_list(pg, doc_ids, n, "read")) return rc;
-  if (dtype != CHIMERA_F32 && dtype != CHIMERA_BF16) return fail(CHIMERA_E_INVAL, "dtype must be F32 or BF16");
-  if ((uintptr_t)out % 16) return fail(CHIMERA_E_INVAL, "read: out must be 16-byte aligned");
-  hipStream_t s = (hipStream_t)hip_stream;
-  BusyGuard<chimera_pages> bg(pg);
-  if (!bg.ok) return fail(CHIMERA_E_BUSY, "pages in use by another thread");
-  DeviceGuard dg(pg->device);
-  if (!dg.ok) return fail(CHIMERA_E_DEVICE, "cannot select device %d", pg->device);
-  return guarded([&]() -> int {
-    int64_t at = 0, items = 0, total = 0;
-    if (BookError e = pg->book.check_read(doc_ids, n, &at, &items, &total); e != BookError::none)
-      return book_fail(e, "read", doc_ids, at);
-    if (total > rows)
-      return fail(CHIMERA_E_INVAL, "read: %lld tokens, out has %lld rows", (long long)total, (long long)rows);
-    if (items == 0) return CHIMERA_OK;
-    if (!out) return fail(CHIMERA_E_INVAL, "null output pointer");
-    if (items > kPagesMaxItems) return fail(CHIMERA_E_UNSUPPORTED, "read: too many tokens in one call");
-    if (int rc = check_stream(s, "read")) return rc;
-    char *plan = nullptr;
-    if (int rc = pages_order_before(pg, s)) return rc;
-    if (int rc = ring_take(pg, (size_t)items * sizeof(PageItem), s, &plan)) return rc;
-    pg->book.plan_read(doc_ids, n, (PageItem *)plan);
-    const PageItem *it = (const PageItem *)plan_for_device(pg, plan, (size_t)items * sizeof(PageItem), s);
-    launch_pages_read(it, items, pg->view.pool, pg->view.table, pg->view.stride, out, dtype, s);
-    CHIMERA_HIP(hipGetLastError());
-    return pages_order_after(pg, s);
-  });
+  return read_common(pg, doc_ids, n, out, rows, dtype, nullptr, hip_stream);
+}
+
+int chimera_pages_read_all(chimera_pages *pg, const int64_t *doc_ids, int64_t n, void *out, int64_t rows, int dtype,
+                           int64_t *total, void *hip_stream) {
+  if (!total) return fail(CHIMERA_E_INVAL, "read: null total");
+  return read_common(pg, doc_ids, n, out, rows, dtype, total, hip_stream);
 }
 
 int chimera_pages_score(chimera_pages *pg, const void *Q, int q_dtype, int64_t nq, int32_t Tq, int32_t d,

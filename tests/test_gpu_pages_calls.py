@@ -120,3 +120,84 @@ def _written(call, out):
         here = torch.arange(cand.shape[1], device="cuda") < n[:, None]
         return cand[here], keys[here], n
     return out
+
+
+# ------------------------------------------------------------ other threads
+class _Between:
+    """The library of a store; before each call but the first, `change` runs (another thread's call there)."""
+
+    def __init__(self, library, change):
+        self.library, self.change, self.calls = library, change, 0
+
+    def __getattr__(self, name):
+        def call(*a):
+            self.calls += 1
+            if self.calls > 1:
+                self.change()
+            return getattr(self.library, name)(*a)
+        return call
+
+
+@pytest.mark.parametrize("change", ["drop", "shorten", "extend", "nothing left", "from nothing"])
+@pytest.mark.parametrize("given", [False, True])
+def test_a_read_while_another_thread_changes_the_documents(change, given):
+    """A read whose documents change between counting and reading is refused, and leaves what it was given alone."""
+    rng = np.random.default_rng(51)
+    x = units(rng, 90)
+    X, v = tensor(x), mx_values(x)
+    pg = Pages(12, 4, 60)
+    empty = change == "from nothing"
+    if not empty:
+        pg.append([1, 2], X[:60], [40, 20])
+    L, ids = pg._lib, np.array([1, 2], np.int64)
+
+    def run():
+        pg._lib = L
+        if change == "drop":
+            pg.drop([2])
+        elif change == "nothing left":
+            pg.drop([1, 2])
+        elif change == "shorten":
+            pg.copy([1], [1], [17])
+        else:
+            pg.append([2], X[60:69], [9])
+
+    before = torch.full((0 if empty else 60, 128), 7.0, device="cuda")
+    pg._lib = _Between(L, run)
+    say("read while", change)
+    _refused(chimera.E_INVAL, pg.read, ids, **({"out": before} if given else {}))
+    pg._lib = L
+    torch.cuda.synchronize()
+    assert torch.all(before == 7.0)
+    want = {"drop": [v[:40]], "nothing left": [v[:0]], "shorten": [v[:17], v[40:60]],
+            "extend": [v[:60], v[60:69]], "from nothing": [v[60:69]]}[change]
+    same(pg.read([1, 2]), np.concatenate(want))
+
+
+def test_read_all_through_the_c_entry():
+    import ctypes
+    rng = np.random.default_rng(52)
+    x = units(rng, 53)
+    pg = Pages(5, 3, 33)
+    pg.append([0, 1], tensor(x), [20, 33])
+    L, h, ids, total = pg._lib, pg._h, (ctypes.c_int64 * 3)(1, 0, 2), ctypes.c_int64(-5)
+    out, s = torch.full((60, 128), 7.0, device="cuda"), torch.cuda.current_stream().cuda_stream
+
+    def read(n, rows, at=None):
+        total.value = -5
+        return L.chimera_pages_read_all(h, ids, n, out.data_ptr() if at is None else at, rows, chimera.F32,
+                                        ctypes.byref(total), s), total.value
+
+    assert read(3, -1, 0) == (0, 53) and read(1, -1, 0) == (0, 33) and read(0, -1, 0) == (0, 0)
+    assert read(3, 54) == (chimera.E_INVAL, 53) and read(3, 52) == (chimera.E_INVAL, 53)
+    assert read(3, 0) == (chimera.E_INVAL, 53) and read(3, 53, 0) == (chimera.E_INVAL, 53)
+    ids[2] = 3
+    assert read(3, 53) == (chimera.E_INVAL, -5)
+    ids[2] = 2
+    torch.cuda.synchronize()
+    assert torch.all(out == 7.0)
+    assert read(3, 53) == (0, 53)
+    same(out[:53], mx_values(np.concatenate([x[20:], x[:20]])))
+    assert torch.all(out[53:] == 7.0)
+    assert L.chimera_pages_read(h, ids, 3, out.data_ptr(), 60, chimera.F32, s) == 0  # the other one takes more rows
+    assert L.chimera_pages_read_all(h, ids, 3, out.data_ptr(), 53, chimera.F32, None, s) == chimera.E_INVAL

@@ -66,3 +66,10 @@ def test_lengths_of_a_copy_are_checked_before_its_positions_are_read(tmp_path):
                            os.path.join(HERE, "pages_copy_lengths.cpp")])
     r = subprocess.run([exe], capture_output=True, text=True, timeout=100)
     assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout
+
+
+def test_read_all_refuses_null_arguments_without_gpu():
+    L, one, total = chimera.lib(), (ctypes.c_int64 * 1)(0), ctypes.c_int64(7)
+    assert L.chimera_pages_read_all(None, one, 1, None, -1, chimera.BF16, ctypes.byref(total), None) == chimera.E_INVAL
+    assert L.chimera_pages_read_all(None, one, 1, None, -1, chimera.BF16, None, None) == chimera.E_INVAL
+    assert total.value == 7
