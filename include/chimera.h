@@ -520,13 +520,13 @@ int chimera_pages_read_all(chimera_pages *pg, const int64_t *doc_ids, int64_t n,
 /* scores device [nq][n] float32: score(i, V) = sum_j max_{t in V} <Q_ij, v_t>
  * over the stored values v of document V = doc_ids[i * ld + c].
  *   Q        device [nq][Tq][128], 16-byte aligned, rounded onto the value grid
- *            as for the searches; finite values
+ *            as for the searches; values that bfloat16 holds as finite ones
  *   doc_ids  device [nq] lists of n ids, ld entries apart (0: one list for
  *            every query); NULL: documents 0 .. n - 1, n <= ndocs
  * An id outside [0, ndocs), an empty document and one whose tokens are all NaN
  * score -infinity; a token with a NaN block is never a document's best.  Query
  * values are used exactly while those of a block of 32 stay below 8 in
- * magnitude (above, to within 2^-15 of the block's largest); products are summed
+ * magnitude (above, to within 2^-14 of the block's largest); products are summed
  * in float32, as are the at most 64 maxima.  Neither scratch nor host
  * synchronisation. */
 int chimera_pages_score(chimera_pages *pg, const void *Q, int q_dtype, int64_t nq, int32_t Tq, int32_t d,

@@ -241,9 +241,11 @@ __global__ __launch_bounds__(256) void k_pages_drop(const int64_t *__restrict__ 
 // k = 32 d1 + d0: up to 512 |d0| <= 16, and above, where bf16 has every fourth k
 // only, d1 is even and d0 a multiple of 4, at most 32.  Larger blocks take three
 // digits |d| <= 16, k = 1024 d2 + 32 d1 + d0; the third one's products are left
-// out for a query that has none.  Blocks of values of 8 or more are shifted right
-// by as many bits as 15 lack: an error of at most 2^-15 of the block's largest
-// value.  Lane l holds query token l % 32 of a block of 32, dimensions
+// out for a query that has none.  Blocks whose largest value is 8 or more are
+// shifted right until its k is below 2^14, and rounded: half a unit, where the
+// largest k is 2^13 units or more, so at most 2^-14 of the block's largest value.
+// The largest finite bf16 shifts by 125, and the third digit's exponent is then
+// the last one that a scale holds.  Lane l holds query token l % 32 of a block of 32, dimensions
 // 64 step + 32 (l / 32) .. + 31.
 struct QueryOperand {
   v6u32 digit[2][2];
@@ -286,7 +288,7 @@ __device__ __forceinline__ bool prepare_query(const QueryRaw<NB, F32> &raw, uint
   bool any = false;
 #pragma unroll
   for (int blk = 0; blk < NB; ++blk) {
-    float k[16];
+    float q[16];
 #pragma unroll
     for (int i = 0; i < (F32 ? 4 : 2); ++i) {
       const uint4 v = raw.v[blk][i];
@@ -294,35 +296,39 @@ __device__ __forceinline__ bool prepare_query(const QueryRaw<NB, F32> &raw, uint
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
         if constexpr (F32) {
-          k[4 * i + m] = __uint_as_float((uint32_t)grid_bf16_bits(__uint_as_float(y[m])) << 16) * 2048.0f;
+          q[4 * i + m] = __uint_as_float((uint32_t)grid_bf16_bits(__uint_as_float(y[m])) << 16);
         } else {
-          // below 1/16 rounded onto the grid; above it every bf16 is on it
-          k[8 * i + 2 * m] = rintf(__uint_as_float(y[m] << 16) * 2048.0f);
-          k[8 * i + 2 * m + 1] = rintf(__uint_as_float(y[m] & 0xFFFF0000u) * 2048.0f);
+          // above 1/16 every bf16 is on the grid; below it k is rounded onto it
+          q[8 * i + 2 * m] = __uint_as_float(y[m] << 16);
+          q[8 * i + 2 * m + 1] = __uint_as_float(y[m] & 0xFFFF0000u);
         }
       }
     }
     float top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(k[i]));
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(q[i]));
     top = fmaxf(top, shfl_xor(top, 1));  // of the block's other half
     f32x16 dig[3][2] = {};  // even and odd dimensions, as the conversion takes them, and as many zeros
     int shift = 0;
-    if (top <= 512.0f) {
+    if (top <= 0.25f) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float a1 = rintf(k[i] * (1.0f / 32.0f));
+        const float k = rintf(q[i] * 2048.0f), a1 = rintf(k * (1.0f / 32.0f));
         dig[1][i & 1][i >> 1] = a1;
-        dig[0][i & 1][i >> 1] = k[i] - 32.0f * a1;
+        dig[0][i & 1][i >> 1] = k - 32.0f * a1;
       }
     } else {
-      const bool wide = top > 1024.0f;
+      const bool wide = top > 0.5f;
       any |= wide;
-      shift = min(max((int)(__float_as_uint(top) >> 23) - 127 - 13, 0), 100);
-      const float down = __uint_as_float((uint32_t)(127 - shift) << 23);
+      shift = min(max((int)(__float_as_uint(top) >> 23) - 127 - 2, 0), 125);
+      // x = k shifted.  A large k is no float, so from 9 bits on the shift comes
+      // first: values below 1/16 are rounded to 0 either way, others are on the grid.
+      const int first = shift > 8 ? shift : 0;
+      const float up = __uint_as_float((uint32_t)(127 + 11 - first) << 23);
+      const float down = __uint_as_float((uint32_t)(127 + first - shift) << 23);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float x = rintf(k[i] * down);
+        const float x = rintf(rintf(q[i] * up) * down);
         const float a2 = wide ? rintf(x * (1.0f / 1024.0f)) : 0.0f, r = x - 1024.0f * a2;
         const float a1 = fabsf(r) > 512.0f ? 2.0f * rintf(r * (1.0f / 64.0f)) : rintf(r * (1.0f / 32.0f));
         dig[2][i & 1][i >> 1] = a2;

@@ -9,7 +9,7 @@ import synth
 from paper_2608_23553_amd import ChimeraError, Pages, chimera
 from util_build import product_builder
 from util_gpu import q_tensor, say, setup
-from util_pages import check_scores, host, mx_values, same, tensor, units
+from util_pages import check_scores, grid, host, mx_values, same, tensor, units
 
 pytestmark = pytest.mark.gpu
 
@@ -201,3 +201,76 @@ def test_read_all_through_the_c_entry():
     assert torch.all(out[53:] == 7.0)
     assert L.chimera_pages_read(h, ids, 3, out.data_ptr(), 60, chimera.F32, s) == 0  # the other one takes more rows
     assert L.chimera_pages_read_all(h, ids, 3, out.data_ptr(), 53, chimera.F32, None, s) == chimera.E_INVAL
+
+
+# ------------------------------------------------------------ queries of any magnitude
+def _magnitudes(rng, n, lo=-12):
+    """n queries [1, 128]: blocks whose largest values go from 2^lo to the largest of bfloat16, others down to 2^-19 of
+    them."""
+    q = rng.uniform(-1, 1, (n, 4, 32)) * 2.0 ** -rng.integers(0, 20, (n, 4, 32))
+    q[:, :, rng.integers(0, 32)] = rng.uniform(1, 2, (n, 4))
+    e = np.resize(np.arange(lo, 128), 4 * n).reshape(n, 4)
+    return np.clip(q * 2.0 ** e[..., None], -3.38e38, 3.38e38).reshape(n, 1, 128).astype(np.float32)
+
+
+def _lost(q):
+    """How far the value used for a query value may be off [.., 128]: nothing below 8, above a half of a unit of which
+    the block's largest value has 2^13 or more."""
+    top = np.abs(q).reshape(*q.shape[:-1], 4, 32).max(-1)
+    return np.where(top >= 8, top * 2.0**-14, 0.0).repeat(32, -1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("form", ["shared", "own lists", "one at a time"])
+def test_query_values_of_every_magnitude(form, dtype):
+    """Documents of one value 1: a score is the value used for the query's, which is a sum of a few exact terms."""
+    rng = np.random.default_rng(61)
+    eye = np.zeros((128, 128), np.float32)
+    eye[np.arange(128), np.arange(128)] = 1
+    pg = Pages(128, 128, 1)
+    pg.append(np.arange(128), tensor(eye), [1] * 128)
+    q = _magnitudes(rng, 140)
+    q[0, 0, :5] = [8, 2.0**-11, 3 * 2.0**-11, 5, -7.96875]
+    q[0, 0, 5:32] = 0
+    Q = tensor(q, dtype)
+    say("query values", form, dtype)
+    if form == "own lists":
+        got = pg.score(Q, torch.arange(128, dtype=torch.int32, device="cuda").repeat(len(q), 1))
+    elif form == "shared":
+        got = pg.score(Q)
+    else:
+        got = torch.cat([pg.score(x[None]) for x in Q])
+    got, want = got.cpu().double().numpy(), grid(Q)[:, 0]
+    off = np.abs(got - want)
+    bad = ~(off <= _lost(want))
+    assert not bad.any(), (np.argwhere(bad)[:3], got[bad][:3], want[bad][:3])
+    assert (got[np.abs(want).reshape(-1, 4, 32).max(-1).repeat(32, -1) < 8].size > 1000)
+
+
+@pytest.mark.parametrize("e", [0, 3, 13, 60, 101, 102, 103, 106, 110, 117, 120, 125, 127])
+@pytest.mark.parametrize("Tq", [5, 40])
+def test_large_queries_and_small_documents(e, Tq):
+    """Scores of ordinary size from queries up to the largest there are: all blocks of a query near 2^e, then only some."""
+    rng = np.random.default_rng(62)
+    x = rng.standard_normal((60, 128)) * 2.0**-e
+    X = tensor(x)
+    pg = Pages(6, 3, 30)
+    pg.append([0, 1, 2], X, [10, 20, 30])
+    v = mx_values(host(X))
+    docs = [v[:10], v[10:30], v[30:]]
+    q = rng.uniform(-1.98, 1.98, (3, Tq, 128)) * 2.0**e
+    q[1, :, :64] *= 2.0**-e
+    q[2, ::2] *= 2.0**-e
+    Q = tensor(q)
+    say("large queries", e, Tq)
+    got = pg.score(Q).cpu().numpy()
+    for i, g in enumerate(grid(Q)):
+        top = np.abs(g).reshape(Tq, 4, 32).max(-1).repeat(32, -1)
+        for d in range(3):
+            a = np.abs(docs[d])
+            # Each product is exact and each of 3 * 128 additions rounds by half a step of a partial sum.  The lower
+            # digits are at most 2 * (512 + 16) units of 2^-11 below 8 (0.516), and of 2^-13 of the largest value above.
+            A = ((np.abs(g) + np.maximum(0.516, 0.129 * top)) @ a.T).max(1).sum()
+            tol = 2.0**-24 * (384 + Tq) * A + (_lost(g) @ a.T).max(1).sum()
+            want = (g @ docs[d].T).max(1).sum()
+            assert abs(got[i, d] - want) <= tol, (i, d, got[i, d], want, tol)
