@@ -12,18 +12,28 @@
 
 namespace chimera {
 
-static bool capturing(hipStream_t s) {
+// Whether s is being captured into a graph.  Elsewhere: another stream is, and
+// that forbids work on this one (the null stream beside a blocking stream).
+enum class Capture { none, here, elsewhere };
+static Capture capture(hipStream_t s) {
   hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
   if (hipStreamIsCapturing(s, &st) != hipSuccess) {
     (void)hipGetLastError();
-    return true;  // another stream's capture forbids work on this one
+    return Capture::elsewhere;
   }
-  return st != hipStreamCaptureStatusNone;
+  return st == hipStreamCaptureStatusNone ? Capture::none : Capture::here;
+}
+static int captured_elsewhere(const char *call) {
+  return fail(CHIMERA_E_UNSUPPORTED, "%s: another stream's capture forbids work on this one", call);
 }
 
 int pages_not_captured(hipStream_t s, const char *call, const char *why) {
-  if (capturing(s)) return fail(CHIMERA_E_UNSUPPORTED, "%s: cannot be captured into a graph (%s)", call, why);
-  return CHIMERA_OK;
+  switch (capture(s)) {
+    case Capture::none: return CHIMERA_OK;
+    case Capture::elsewhere: return captured_elsewhere(call);
+    case Capture::here: break;
+  }
+  return fail(CHIMERA_E_UNSUPPORTED, "%s: cannot be captured into a graph (%s)", call, why);
 }
 
 int pages_order_before(chimera_pages *pg, hipStream_t s) {
@@ -439,7 +449,9 @@ int chimera_pages_score(chimera_pages *pg, const void *Q, int q_dtype, int64_t n
   if (!bg.ok) return fail(CHIMERA_E_BUSY, "pages in use by another thread");
   DeviceGuard dg(pg->device);
   if (!dg.ok) return fail(CHIMERA_E_DEVICE, "cannot select device %d", pg->device);
-  const bool graph = capturing(s);
+  const Capture c = capture(s);
+  if (c == Capture::elsewhere) return captured_elsewhere("score");
+  const bool graph = c == Capture::here;
   if (!graph)
     if (int rc = pages_order_before(pg, s)) return rc;
   launch_pages_score(Q, q_dtype, nq, Tq, Tq, doc_ids, ld, nullptr, n, pg->view, scores, false, s);

@@ -1,6 +1,8 @@
 """Calls on the paged store that its other tests do not make: a search where it
 cannot be, tensors of another stream, another thread between two calls, queries
 of any magnitude, plans that go round their buffers."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -60,6 +62,45 @@ def test_a_search_in_a_capture_is_refused(before):
             same(pg.read([5]), v[:7])
     pg.drop([3, 4, 5])
     assert pg.info()["ntokens"] == 0
+
+
+def _hip():
+    """The HIP runtime that torch has loaded."""
+    with open("/proc/self/maps") as f:
+        return ctypes.CDLL(next(line.split()[-1] for line in f if "libamdhip64" in line))
+
+
+def test_calls_on_the_null_stream_while_a_blocking_stream_is_captured():
+    """Work on the null stream would end such a capture: every call is refused and queues nothing, and all is well
+    after it."""
+    w, c, kk, cl, oi, idx = setup("tiny")
+    q, _ = c.queries(2, w.Tq)
+    Q = q_tensor(q, "bf16")
+    rng = np.random.default_rng(32)
+    x = units(rng, 50)
+    X, v = tensor(x), mx_values(x)
+    pg = Pages(1000, 1000, 64)
+    pg.append([1, 2], X, [20, 30])
+    out, rows = torch.full((2, 1000), 7.0, device="cuda"), torch.full((50, 128), 7.0, device="cuda")
+    res = idx.search_pages(pg, Q, w.nprobe, w.ncand, 5)
+    info = pg.info()
+    torch.cuda.synchronize()
+    H, s, g = _hip(), ctypes.c_void_p(), ctypes.c_void_p()
+    assert torch.cuda.current_stream().cuda_stream == 0
+    assert H.hipStreamCreateWithFlags(ctypes.byref(s), 0) == 0 and H.hipStreamBeginCapture(s, 2) == 0
+    try:
+        for f in (lambda: pg.score(Q, out=out), lambda: pg.append([3], X, [50]), lambda: pg.drop([1]),
+                  lambda: pg.read([1, 2], out=rows), lambda: pg.fork([1], [4]), lambda: pg.copy([1], [4]),
+                  lambda: idx.search_pages(pg, Q, w.nprobe, w.ncand, 5, out=res)):
+            _refused(chimera.E_UNSUPPORTED, f)
+    finally:
+        ended = H.hipStreamEndCapture(s, ctypes.byref(g))
+    assert ended == 0 and H.hipGraphDestroy(g) == 0 and H.hipStreamDestroy(s) == 0
+    torch.cuda.synchronize()
+    assert torch.all(out == 7.0) and torch.all(rows == 7.0) and pg.info() == info
+    same(pg.read([1, 2]), v)
+    pg.score(Q, out=out)
+    check_scores(out[:, :4], Q, [v[:0], v[:20], v[20:], v[:0]], [range(4)] * 2)
 
 
 # ------------------------------------------------------------ streams
@@ -175,7 +216,6 @@ def test_a_read_while_another_thread_changes_the_documents(change, given):
 
 
 def test_read_all_through_the_c_entry():
-    import ctypes
     rng = np.random.default_rng(52)
     x = units(rng, 53)
     pg = Pages(5, 3, 33)
