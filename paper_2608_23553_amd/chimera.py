@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import operator
 import os
 from typing import Callable, Iterable, Tuple
 
@@ -376,6 +377,7 @@ class Index:
 
     def search_pages(self, pages: "Pages", Q, nprobe: int, ncand: int, k: int, out=None, stream=None):
         """chimera_search_pages: step 4 scored from a paged store's documents of the same ids."""
+        nprobe, ncand, k = _whole(nprobe, "nprobe"), _whole(ncand, "ncand"), _whole(k, "k")
         Q, dt = self._q(Q, stream)
         nq, Tq, d = Q.shape
         ids, scores = self._results(Q, nq, k, out, stream)
@@ -523,6 +525,14 @@ def _counts(a, n: int | None, name: str) -> np.ndarray:
     return b if b.flags.c_contiguous else np.ascontiguousarray(b)
 
 
+def _whole(v, name: str, bits: int = 32) -> int:
+    """A size as a signed number of so many bits; one that they do not hold is an error, not another size."""
+    v = operator.index(v)
+    if not -(1 << bits - 1) <= v < 1 << bits - 1:
+        raise ValueError(f"{name} must be a whole number of {bits} bits")
+    return v
+
+
 _BYTES = ctypes.c_char * 1
 
 
@@ -547,6 +557,8 @@ class Pages:
     def __init__(self, npages: int, ndocs: int, max_len: int, device: int = 0):
         import torch
         h = ctypes.c_void_p()
+        npages, ndocs = _whole(npages, "npages", 64), _whole(ndocs, "ndocs", 64)
+        max_len, device = _whole(max_len, "max_len"), _whole(device, "device")
         self._lib = lib()
         _check(self._lib.chimera_pages_create(device, npages, ndocs, max_len, ctypes.byref(h)))
         self._h = h

@@ -7,7 +7,7 @@ import subprocess
 import numpy as np
 import pytest
 
-from paper_2608_23553_amd import ChimeraError, Pages, chimera
+from paper_2608_23553_amd import ChimeraError, Index, Pages, chimera
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -73,3 +73,21 @@ def test_read_all_refuses_null_arguments_without_gpu():
     assert L.chimera_pages_read_all(None, one, 1, None, -1, chimera.BF16, ctypes.byref(total), None) == chimera.E_INVAL
     assert L.chimera_pages_read_all(None, one, 1, None, -1, chimera.BF16, None, None) == chimera.E_INVAL
     assert total.value == 7
+
+
+@pytest.mark.parametrize("npages,ndocs,max_len,device", [
+    (2**64 + 1, 1, 1, 0), (1, 2**64 + 1, 1, 0), (1, 1, 2**32 + 1, 0), (1, 1, 1, 2**32), (1, 1, -2**32 + 1, 0),
+    (2**63, 1, 1, 0), (1, 1, 2**31, 0)])
+def test_sizes_that_the_library_cannot_be_told(npages, ndocs, max_len, device):
+    """Not taken for what is left of them in 32 or 64 bits."""
+    with pytest.raises(ValueError):
+        Pages(npages, ndocs, max_len, device)
+    with pytest.raises(TypeError):
+        Pages(1.5, 1, 1)
+
+
+@pytest.mark.parametrize("nprobe,ncand,k", [(2**32 + 2, 256, 10), (2, 2**32 + 256, 10), (2, 256, 2**32 + 10),
+                                            (2, 256, 2**31), (2, 256, -2**32 + 10)])
+def test_a_search_from_pages_with_sizes_that_the_library_cannot_be_told(nprobe, ncand, k):
+    with pytest.raises(ValueError, match="32 bits"):
+        Index.search_pages(Index.__new__(Index), None, None, nprobe, ncand, k)
