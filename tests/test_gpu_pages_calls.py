@@ -314,3 +314,61 @@ def test_large_queries_and_small_documents(e, Tq):
             tol = 2.0**-24 * (384 + Tq) * A + (_lost(g) @ a.T).max(1).sum()
             want = (g @ docs[d].T).max(1).sum()
             assert abs(got[i, d] - want) <= tol, (i, d, got[i, d], want, tol)
+
+
+# ------------------------------------------------------------ views and plans
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("first", [1, 2, 4, 8, 31])
+def test_rows_of_a_wider_tensor_at_any_offset(dtype, first):
+    """Views whose rows begin at `first` of 192 values, padded and packed: what the library cannot take is copied."""
+    rng = np.random.default_rng(71)
+    lens = np.array([5, 0, 33, 40, 1], np.int32)
+    wide = tensor(units(rng, 300).reshape(-1, 192), dtype).view(5, 40, 192)
+    X = wide[..., first:first + 128]
+    v = mx_values(host(X).reshape(-1, 128)).reshape(5, 40, 128)
+    want = np.concatenate([v[i, :n] for i, n in enumerate(lens)])
+    for name, t in (("padded", X), ("one document", X[3:4]), ("packed", wide.view(-1, 192)[:79, first:first + 128])):
+        pg = Pages(20, 5, 40)
+        if name == "padded":
+            pg.append(np.arange(5), t, lens)
+            same(pg.read(np.arange(5)), want, name)
+        elif name == "one document":
+            pg.append([2], t, [37])
+            same(pg.read([2]), v[3, :37], name)
+        else:
+            pg.append(np.arange(5), t, lens)
+            same(pg.read(np.arange(5)), v.reshape(-1, 128)[:79], name)
+
+
+@pytest.mark.parametrize("n", [300, 3000])
+def test_plans_that_go_round_their_buffers(n):
+    """Plans of several times the buffers (half a MiB each), read in place (300 documents) and copied (3,000), on two
+    streams and the null stream, with nothing waited for in between."""
+    rng = np.random.default_rng(72)
+    x = units(rng, 64)
+    X, v = tensor(x), mx_values(x)
+    pg = Pages(3 * n, 2 * n, 40)
+    a, b = np.arange(n), np.arange(n, 2 * n)
+    streams = [torch.cuda.Stream(), None, torch.cuda.Stream()]
+    rows = torch.arange(n, device="cuda") % 64
+    batches = [X.roll(k, 0)[rows] for k in range(5)]
+    lists = [np.roll(v, k, 0)[np.arange(n) % 64] for k in range(5)]
+    torch.cuda.synchronize()
+    ones = np.ones(n, np.int32)
+    rounds = -(-5 * (512 << 10) // (32 * 4 * n))  # each makes 4 plans of 32 bytes a document or more
+    reads, wants = [], []
+    for k in range(rounds):
+        s = streams[k % 3]
+        pg.drop(a, stream=s)
+        pg.append(a, batches[k % 5], ones, stream=streams[(k + 1) % 3])
+        pg.append(a, batches[(k + 1) % 5], ones, stream=s)
+        pg.drop(b, stream=streams[(k + 2) % 3])
+        pg.fork(a, b, 1 + (a + k) % 2, stream=s)
+        if k % 8 == 7 or k == rounds - 1:
+            reads.append(pg.read(np.stack([a, b], 1).reshape(-1), stream=streams[(k + 2) % 3]))
+            both = np.stack([lists[k % 5], lists[(k + 1) % 5]], 1)
+            wants.append(np.concatenate([r for i in range(n) for r in (both[i], both[i, :1 + (i + k) % 2])]))
+    torch.cuda.synchronize()
+    say("rounds", rounds, "reads", len(reads))
+    for i, (r, want) in enumerate(zip(reads, wants)):
+        same(r, want, f"read {i}")
