@@ -667,15 +667,16 @@ class Pages:
         import torch
         a = _ids(ids)
         total = ctypes.c_int64()
-        _check(self._lib.chimera_pages_read_all(self._h, _at(a), a.size, None, -1, BF16, ctypes.byref(total), None))
+        at, n, count = _at(a), a.size, ctypes.byref(total)
+        _check(self._lib.chimera_pages_read_all(self._h, at, n, None, -1, BF16, count, None))
         rows = total.value
         if out is None:
             with _on(stream):
                 out = torch.empty((rows, 128), dtype=dtype or torch.bfloat16, device=self.device)
         elif tuple(out.shape) != (rows, 128) or not out.is_contiguous() or (dtype is not None and out.dtype != dtype):
             raise ValueError(f"out must be a contiguous tensor [{rows}, 128]{'' if dtype is None else f' of {dtype}'}")
-        _check(self._lib.chimera_pages_read_all(self._h, _at(a), a.size, out.data_ptr(), rows, self._type(out, "out"),
-                                                ctypes.byref(total), self._stream(stream)))
+        _check(self._lib.chimera_pages_read_all(self._h, at, n, out.data_ptr(), rows, self._type(out, "out"), count,
+                                                self._stream(stream)))
         return out
 
     def score(self, Q, ids=None, out=None, stream=None):

@@ -142,8 +142,8 @@ static int check_stream(hipStream_t s, const char *call) {
   return pages_not_captured(s, call, "its host bookkeeping happens once");
 }
 
-// exact: the documents' tokens, which have to be as many as rows (below 0: nothing
-// is read); null: at most as many.
+// exact: the documents' tokens, which have to be as many as rows (below 0: they
+// are only counted); null: at most as many.
 static int read_common(chimera_pages *pg, const int64_t *doc_ids, int64_t n, void *out, int64_t rows, int dtype,
                        int64_t *exact, void *hip_stream) {
   if (int rc = check_list(pg, doc_ids, n, "read")) return rc;
@@ -152,14 +152,14 @@ static int read_common(chimera_pages *pg, const int64_t *doc_ids, int64_t n, voi
   hipStream_t s = (hipStream_t)hip_stream;
   BusyGuard<chimera_pages> bg(pg);
   if (!bg.ok) return fail(CHIMERA_E_BUSY, "pages in use by another thread");
+  int64_t at = 0, items = 0, total = 0;
+  if (exact && rows < 0) return book_fail(pg->book.count(doc_ids, n, &at, exact), "read", doc_ids, at);
   DeviceGuard dg(pg->device);
   if (!dg.ok) return fail(CHIMERA_E_DEVICE, "cannot select device %d", pg->device);
   return guarded([&]() -> int {
-    int64_t at = 0, items = 0, total = 0;
     if (BookError e = pg->book.check_read(doc_ids, n, &at, &items, &total); e != BookError::none)
       return book_fail(e, "read", doc_ids, at);
     if (exact) *exact = total;
-    if (exact && rows < 0) return CHIMERA_OK;
     if (total > rows || (exact && total < rows))
       return fail(CHIMERA_E_INVAL, "read: %lld tokens, out has %lld rows", (long long)total, (long long)rows);
     if (items == 0) return CHIMERA_OK;

@@ -312,14 +312,23 @@ struct PageBook {
   }
 
   // ---- read: the tokens of ids[i], one document behind the other
-  BookError check_read(const int64_t *ids, int64_t n, int64_t *at, int64_t *items, int64_t *rows) const {
-    *items = *rows = 0;
+  BookError count(const int64_t *ids, int64_t n, int64_t *at, int64_t *rows) const {
+    int64_t sum = 0;
     for (int64_t i = 0; i < n; ++i) {
-      *at = i;
-      if (ids[i] < 0 || ids[i] >= ndocs) return BookError::id;
-      *items += (pages_of(len[ids[i]]) + kItemPages - 1) / kItemPages;
-      *rows += len[ids[i]];
+      if (ids[i] < 0 || ids[i] >= ndocs) {
+        *at = i;
+        return BookError::id;
+      }
+      sum += len[ids[i]];
     }
+    *rows = sum;
+    return BookError::none;
+  }
+  BookError check_read(const int64_t *ids, int64_t n, int64_t *at, int64_t *items, int64_t *rows) const {
+    if (BookError e = count(ids, n, at, rows); e != BookError::none) return e;
+    int64_t sum = 0;
+    for (int64_t i = 0; i < n; ++i) sum += (uint32_t)(len[ids[i]] + kItemPages * kPageTokens - 1) / (kItemPages * kPageTokens);
+    *items = sum;
     return BookError::none;
   }
   void plan_read(const int64_t *ids, int64_t n, PageItem *item) const {
