@@ -535,7 +535,7 @@ int chimera_pages_score(chimera_pages *pg, const void *Q, int q_dtype, int64_t n
 /* chimera_search with step 4 scored from a paged store: the kept documents of
  * the index are ranked by score(i, V) of the documents of the same ids in pg
  * (same device; pg's ndocs >= the index's), through the keys rint(score 2^22)
- * (saturating at +-2^31); scores are key * 2^-22 in float32.  Kept documents
+ * (saturating at +-(2^31 - 128)); scores are key * 2^-22 in float32.  Kept documents
  * that score -infinity (no tokens in pg) are left out: the results end in
  * (-1, -INFINITY) there. */
 int chimera_search_pages(chimera_index *idx, chimera_pages *pg, const void *Q, int q_dtype, int64_t nq, int32_t Tq,

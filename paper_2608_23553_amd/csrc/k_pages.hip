@@ -435,8 +435,8 @@ __device__ __forceinline__ f32x16 page_products(const PageOperand &a, const Quer
 }
 
 // Key of a score, as the searches rank them: rint(F * 2^22), saturated at the
-// largest floats inside the range, so that the lowest key, -2^31, means
-// -infinity alone.
+// largest floats inside the range, +-(2^31 - 128), so that the lowest key, -2^31,
+// means -infinity alone.
 __device__ __forceinline__ int32_t score_key(float F) {
   const float x = rintf(F * KEY_SCALE);
   return F == -INFINITY ? INT32_MIN : (int32_t)fminf(fmaxf(x, -2147483520.0f), 2147483520.0f);
@@ -468,12 +468,15 @@ __global__ __launch_bounds__(256) void k_pages_unscored(int32_t *__restrict__ id
 // workgroup takes one entry, its waves a quarter of the pages each, and their
 // maxima meet in LDS.
 //
-// What bounds it: with a list for each query the reads that miss L2 (256 x 2048
-// entries of 50,000 documents of 64 tokens: 246 us, 1.79 GB at 7.2 TB/s); with
-// one list for many the matrix cores at the clock that their power allows (64
-// queries x 30,000 documents: 523 us, 1.9 PFLOP/s of useful work, cores busy 51%
-// of the cycles); for few entries the chain of list, length, page table and page
-// (100 documents: 7 us).
+// What it measured, and what is known of its bound.  With a list for each query:
+// reads that miss L2 (256 x 2048 entries of 50,000 documents of 64 tokens: 245 us,
+// 1.79 GB at 7.3 TB/s).  With one list for many (64 queries x 30,000 documents:
+// 520 to 545 us, 1.9 PFLOP/s of useful work): the matrix cores are busy 52% of the
+// cycles, at a clock of about 1.9 GHz.  What keeps them idle for the rest is not
+// established: other vector instructions take about a third of the cycles, there
+// are 2.5 waves a SIMD, and a wave waits 43% of its time to issue and 23% for data.
+// For few entries: the chain of list, length, page table and page (100 documents: 7
+// us).
 constexpr int DEPTH = 2, FLUSH = 16, RING = 32;
 static_assert(FLUSH + 2 * DEPTH <= RING, "documents that end within DEPTH tiles have room");
 

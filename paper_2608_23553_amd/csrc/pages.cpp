@@ -102,8 +102,9 @@ static int ring_take(chimera_pages *pg, size_t bytes, hipStream_t s, char **out)
 }
 
 // Where the kernels read the first `bytes` of a plan: in place or, from 32 KB on,
-// copied (1024 items of 48 bytes: 5.4 us copied and read, 6.4 in place; 4096: 8.9
-// and 16.8; 64: 5.2 and 2.8).
+// copied, which is one more launch for the host (2.7 us). On the device, 32 bytes
+// a fork: 256 copied and read 5.4 us, in place 4.4; 512: 5.7 and 6.0; 1024: 6.3 and
+// 9.0; 4096: 9.0 and 26.9; 36 bytes an append: 256: 5.8 and 5.5; 1024: 6.8 and 10.4.
 static char *plan_for_device(chimera_pages *pg, char *plan, size_t bytes, hipStream_t s) {
   if (bytes < (32 << 10)) return plan;
   char *dev = pg->ring.dev + (plan - pg->ring.host);

@@ -326,8 +326,9 @@ struct PageBook {
   }
   BookError check_read(const int64_t *ids, int64_t n, int64_t *at, int64_t *items, int64_t *rows) const {
     if (BookError e = count(ids, n, at, rows); e != BookError::none) return e;
+    constexpr uint32_t kItemTokens = kItemPages * kPageTokens;
     int64_t sum = 0;
-    for (int64_t i = 0; i < n; ++i) sum += (uint32_t)(len[ids[i]] + kItemPages * kPageTokens - 1) / (kItemPages * kPageTokens);
+    for (int64_t i = 0; i < n; ++i) sum += (len[ids[i]] + kItemTokens - 1) / kItemTokens;
     *items = sum;
     return BookError::none;
   }
