@@ -256,13 +256,15 @@ def _on(stream):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
-def _q_args(Q):
+def _q_args(Q, stream):
     import torch
     if not Q.is_cuda:
         raise ValueError("Q must be a device tensor")
     if Q.dim() != 3:
         raise ValueError("Q must be [nq, Tq, d]")
-    Q = Q.contiguous()
+    if not Q.is_contiguous():
+        with _on(stream):
+            Q = Q.contiguous()
     if Q.dtype == torch.float32:
         dt = F32
     elif Q.dtype == torch.bfloat16:
@@ -313,8 +315,7 @@ class Index:
     def _q(self, Q, stream):
         """Q as the library takes it, on the index's own GPU (the library
         receives a bare device pointer and cannot check that)."""
-        with _on(stream):
-            Q, dt = _q_args(Q)
+        Q, dt = _q_args(Q, stream)
         if Q.device.index != self._info["device"]:
             raise ValueError(f"Q is on {Q.device}, the index on cuda:{self._info['device']}")
         return Q, dt
