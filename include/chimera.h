@@ -447,7 +447,8 @@ int chimera_search_collab_rabitq(chimera_index *idx, const void *Q, int q_dtype,
  *    from call to call); a captured score and its replays are not ordered by
  *    the library: the caller keeps them apart from calls that change the
  *    store and run on other streams.  A replay scores the documents as they
- *    are when it runs.
+ *    are when it runs.  E_UNSUPPORTED also where a blocking stream's capture
+ *    forbids work on the null stream, and the call or the one before it is there.
  *  - Concurrent host calls on one store return E_BUSY; info_get and lengths
  *    must not overlap a call that changes the store.  After E_DEVICE the store
  *    must be freed.

@@ -12,8 +12,8 @@
 
 namespace chimera {
 
-// Whether s is being captured into a graph.  Elsewhere: another stream is, and
-// that forbids work on this one (the null stream beside a blocking stream).
+// Whether s is being captured into a graph.  Elsewhere: s is the null stream, and
+// a blocking stream is captured, which forbids work on it.
 enum class Capture { none, here, elsewhere };
 static Capture capture(hipStream_t s) {
   hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
@@ -24,7 +24,7 @@ static Capture capture(hipStream_t s) {
   return st == hipStreamCaptureStatusNone ? Capture::none : Capture::here;
 }
 static int captured_elsewhere(const char *call) {
-  return fail(CHIMERA_E_UNSUPPORTED, "%s: another stream's capture forbids work on this one", call);
+  return fail(CHIMERA_E_UNSUPPORTED, "%s: another stream's capture forbids work on the null stream", call);
 }
 
 int pages_not_captured(hipStream_t s, const char *call, const char *why) {
@@ -39,6 +39,7 @@ int pages_not_captured(hipStream_t s, const char *call, const char *why) {
 int pages_order_before(chimera_pages *pg, hipStream_t s) {
   if (pg->on_null && s == nullptr) return CHIMERA_OK;
   if (pg->on_null) {
+    if (capture(nullptr) != Capture::none) return captured_elsewhere("a call behind work on the null stream");
     CHIMERA_HIP(hipEventRecord(pg->done, nullptr));
     pg->pending = true;
     pg->on_null = false;

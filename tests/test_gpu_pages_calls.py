@@ -102,7 +102,7 @@ def test_calls_on_the_null_stream_while_a_blocking_stream_is_captured():
     pg.append([1, 2], X, [20, 30])
     out, rows = torch.full((2, 1000), 7.0, device="cuda"), torch.full((50, 128), 7.0, device="cuda")
     res = idx.search_pages(pg, Q, w.nprobe, w.ncand, 5)
-    info = pg.info()
+    info, side = pg.info(), torch.cuda.Stream()
     torch.cuda.synchronize()
     H, s, g = _hip(), ctypes.c_void_p(), ctypes.c_void_p()
     assert torch.cuda.current_stream().cuda_stream == 0
@@ -111,7 +111,12 @@ def test_calls_on_the_null_stream_while_a_blocking_stream_is_captured():
         try:
             for f in (lambda: pg.score(Q, out=out), lambda: pg.append([3], X, [50]), lambda: pg.drop([1]),
                       lambda: pg.read([1, 2], out=rows), lambda: pg.fork([1], [4]), lambda: pg.copy([1], [4]),
-                      lambda: idx.search_pages(pg, Q, w.nprobe, w.ncand, 5, out=res)):
+                      lambda: idx.search_pages(pg, Q, w.nprobe, w.ncand, 5, out=res),
+                      # on another stream, which waits for the store's last work, on the null stream
+                      lambda: pg.score(Q, out=out, stream=side), lambda: pg.append([3], X, [50], stream=side),
+                      lambda: pg.drop([1], stream=side), lambda: pg.read([1, 2], out=rows, stream=side),
+                      lambda: pg.fork([1], [4], stream=side), lambda: pg.copy([1], [4], stream=side),
+                      lambda: idx.search_pages(pg, Q, w.nprobe, w.ncand, 5, out=res, stream=side)):
                 _refused(chimera.E_UNSUPPORTED, f)
         finally:
             ended = H.hipStreamEndCapture(s, ctypes.byref(g))
@@ -119,7 +124,8 @@ def test_calls_on_the_null_stream_while_a_blocking_stream_is_captured():
     torch.cuda.synchronize()
     assert torch.all(out == 7.0) and torch.all(rows == 7.0) and pg.info() == info
     same(pg.read([1, 2]), v)
-    pg.score(Q, out=out)
+    pg.score(Q, out=out, stream=side)
+    side.synchronize()
     check_scores(out[:, :4], Q, [v[:0], v[:20], v[20:], v[:0]], [range(4)] * 2)
 
 
